@@ -1,0 +1,100 @@
+/*
+ * C ABI of the library's quantised operators beside the convolutions: products with 4-bit weights, and a cache of
+ * attention keys and values held in 8 bits with the attention that reads it.
+ *
+ * Conventions, in addition to winograd_c.h's (device pointers owned by the caller, no allocation, no synchronisation,
+ * everything enqueued on hip_stream, wg_status codes, validation on the host before the first launch):
+ *   - packed_dev and workspace_dev are 256-byte aligned; 16-bit elements are 2-byte aligned, 32-bit ones 4-byte, the
+ *     cache's four arrays 16-byte.
+ *   - Every call can be captured into a graph: it enqueues kernels only.
+ *   - Results do not depend on the order in which workgroups run.
+ */
+#ifndef QUANTIZED_C_H
+#define QUANTIZED_C_H
+
+#include "winograd_c.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+enum wq_type { WQ_F16 = 0, WQ_BF16 = 1, WQ_I8 = 2, WQ_F32 = 3 };
+
+/* ---- products with 4-bit weights -------------------------------------------------------------------------------
+ *   y[m][n] = act( x_scale[m] * sum_k x[m][k] * scale[n][k / group] * (code[n][k] - zero[n][k / group]) + bias[n] )
+ * codes 0..15, zero points 0..15 (8 where none are given), group 32, 64 or 128, the last group short where group does
+ * not divide K; act is max(0, .) where relu is set.  Sums are held in 32 bits, the result is rounded once. */
+
+/* Size in bytes of the packed blob, header included; 0 if the arguments are invalid. */
+size_t int4_packed_bytes(int N, int K, int group, int has_zeros);
+
+/* Lays codes [N][K] (a byte each, its low four bits count), scales [N][ceil(K / group)] of scale_type WQ_F16 or
+ * WQ_BF16 and zero points [N][ceil(K / group)] (a byte each; NULL = none) out for int4_linear, once per layer. */
+int int4_pack_weights(const uint8_t* codes_dev, const void* scales_dev, int scale_type, const uint8_t* zeros_dev, int N, int K,
+                      int group, void* packed_dev, size_t packed_bytes, void* hip_stream);
+
+/* x: [M][K] of x_type WQ_F16, WQ_BF16 or WQ_I8, rows x_stride elements apart (x_stride >= K).  x_scale: float [M], only for
+ * WQ_I8, or NULL.  bias: float [N] or NULL.  y: dense [M][N] of y_type WQ_F16, WQ_BF16 or WQ_F32.  The blob has to be the one
+ * made for these (N, K, group, scale_type, has_zeros); on a mismatch y is left untouched.  A row of x with an infinite or NaN
+ * element gives NaN in that row. */
+int int4_linear(const void* x_dev, int x_type, long long x_stride, const float* x_scale_dev, const void* packed_dev,
+                const float* bias_dev, void* y_dev, int y_type, int M, int N, int K, int group, int scale_type, int has_zeros,
+                int relu, void* hip_stream);
+
+/* ---- a cache held in 8 bits ------------------------------------------------------------------------------------
+ * A cache holds blocks of `block` (16, 32, 64 or 128) tokens of kv_heads heads of head_dim (64, 128 or 256):
+ *   k  int8 [blocks][kv_heads][block][head_dim],  k_scale float [blocks][kv_heads]
+ *   v  int8 [blocks][kv_heads][head_dim][block],  v_scale float [blocks][kv_heads]
+ * a value being code * scale.  Values lie token by token within a head_dim, because attention sums over tokens there.
+ *
+ * A batch of sequences is told by table int32 [sequences][table_width] (the blocks of a sequence in order), lengths
+ * int32 [sequences] (tokens of a sequence, those of this call included) and starts int32 [sequences + 1]: the rows
+ * starts[b] .. starts[b + 1] - 1 of the call's tensors are the last tokens of sequence b (NULL: one row each).  They are
+ * device memory and read by the kernels: starts and lengths are taken within 0..rows and 0..table_width * block, and a
+ * block number outside 0..blocks - 1 names no block: nothing is stored there, and its tokens are not seen.  Rows behind
+ * starts[sequences], and rows in front of a sequence's first token, are not stored. */
+
+/*
+ * Quantises and stores new keys and values [rows][kv_heads][head_dim] of type WQ_F16 or WQ_BF16 (rows k_stride and
+ * v_stride elements apart, the heads of a row dense).  Of every block and head that receives tokens the scale becomes
+ *   s' = max(s, largest |new| / 127), s the scale before, or 0 where no older token lies in the block,
+ * rounded to float; codes are the nearest integers to value / s' (ties to even) within +-127, and 0 where s' = 0; where
+ * s' > s the older tokens' codes c become the nearest integers to c * s / s'.  Places behind the new tokens keep their
+ * bytes.  NaN is stored as 0, infinity as the type's largest value.  Blocks that receive tokens in one call have to be
+ * different ones.
+ */
+int int8_cache_append(const void* k_dev, long long k_stride, const void* v_dev, long long v_stride, int type, int rows,
+                      int8_t* cache_k_dev, int8_t* cache_v_dev, float* k_scale_dev, float* v_scale_dev, int blocks,
+                      int kv_heads, int head_dim, int block, const int32_t* table_dev, int table_width, int sequences,
+                      const int32_t* lengths_dev, const int32_t* starts_dev, void* hip_stream);
+
+/*
+ * What `count` blocks hold, as values code * scale: out_k and out_v are [count][kv_heads][block][head_dim] of type WQ_F32,
+ * WQ_F16 or WQ_BF16.  ids: int32 [count]; where one names no block its values are 0.
+ */
+int int8_cache_read(const int8_t* cache_k_dev, const int8_t* cache_v_dev, const float* k_scale_dev, const float* v_scale_dev,
+                    int blocks, int kv_heads, int head_dim, int block, const int32_t* ids_dev, int count, void* out_k_dev,
+                    void* out_v_dev, int type, void* hip_stream);
+
+/* Scratch bytes int8_cache_attention needs for calls of these sizes; 0 if it needs none or the arguments are invalid. */
+size_t int8_cache_attention_workspace_bytes(int rows, int heads, int kv_heads, int head_dim, int block, int table_width,
+                                            int sequences, int has_starts);
+
+/*
+ * out[i][h] = sum_t p_t V_t,  p = softmax over the visible tokens t of scale * (q[i][h] . K_t), for the rows of the batch;
+ * head h reads head h / (heads / kv_heads) of the cache.  q and out: [rows][heads][head_dim] of type WQ_F16 or WQ_BF16,
+ * rows q_stride and out_stride elements apart.  A row at position p of its sequence sees the tokens t < lengths[b], where
+ * causal is set only t <= p, and where window > 0 only t > p - window (window needs causal).  A row that sees nothing
+ * becomes 0, and so does a row in front of its sequence's first token; rows behind starts[sequences] are left as they were.
+ * workspace: int8_cache_attention_workspace_bytes(...) bytes, scratch of this call alone while it runs.
+ */
+int int8_cache_attention(const void* q_dev, long long q_stride, int type, int rows, int heads, const int8_t* cache_k_dev,
+                         const int8_t* cache_v_dev, const float* k_scale_dev, const float* v_scale_dev, int blocks, int kv_heads,
+                         int head_dim, int block, const int32_t* table_dev, int table_width, int sequences,
+                         const int32_t* lengths_dev, const int32_t* starts_dev, float scale, int causal, int window, void* out_dev,
+                         long long out_stride, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif

@@ -1,0 +1,99 @@
+// C ABI of the products with 4-bit weights: argument checks on the host, layout of the weights, choice of the kernel.
+#include "int4_weights.h"
+
+namespace wq {
+
+namespace {
+
+bool valid_weights(int N, int K, int group) {
+    return N > 0 && K > 0 && (group == 32 || group == 64 || group == 128);
+}
+
+// Keeps every count an int and every launch below 2^32 threads: 2^34 codes, 2^26 outputs.
+bool too_large(int N, int K) {
+    return N > (1 << 26) || K > (1 << 26) || (long long)ceil_div(N, kTileOutputs) * ceil_div(K, kTileInputs) > (1 << 23);
+}
+
+Int4Weights weights_of(const void* blob, int N, int K, int group, int scale_type, int has_zeros) {
+    const Int4Layout l = int4_layout(N, K, group, has_zeros);
+    const uint8_t* b = static_cast<const uint8_t*>(blob);
+    return {b, b + l.codes, reinterpret_cast<const uint16_t*>(b + l.scales), has_zeros ? b + l.zeros : nullptr,
+            l.output_tiles, l.input_tiles, l.groups, N, K, group, scale_type, has_zeros};
+}
+
+// One thread per word of codes, then one per scale (with its zero point).  Places without an output or an input get code 0 and scale
+// 0: inputs behind the row's end are read as zeros, outputs behind the last are not stored.
+__global__ void int4_pack_kernel(const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, Int4Weights w, uint8_t* blob,
+                                 long long words, long long total) {
+    const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+    if (i == 0) {
+        Int4Header* h = reinterpret_cast<Int4Header*>(blob);
+        h->magic = kInt4Magic; h->version = kInt4Version;
+        h->N = w.N; h->K = w.K; h->group = w.group; h->scale_type = w.scale_type; h->has_zeros = w.has_zeros;
+    }
+    if (i < words) {
+        const int word = (int)(i & 3), lane = (int)(i >> 2) & 63;
+        const long long tile = i >> 8;
+        const long long n = tile / w.input_tiles * kTileOutputs + (lane & 15);
+        const long long k = tile % w.input_tiles * kTileInputs + 32 * word + 8 * (lane >> 4);
+        uint32_t fields = 0;
+        for (int j = 0; j < 8; ++j)
+            if (n < w.N && k + j < w.K) fields |= (uint32_t)(codes[n * w.K + k + j] & 15) << (4 * ((j >> 1) + 4 * (j & 1)));
+        reinterpret_cast<uint32_t*>(const_cast<uint8_t*>(w.codes))[i] = rotate_right(fields, 30);
+    } else if (i < total) {
+        const long long e = i - words;
+        const long long row = e >> 4, n = row / w.groups * kTileOutputs + (e & 15), g = row % w.groups;
+        const int given = ceil_div(w.K, w.group);
+        const bool there = n < w.N && g < given;
+        const_cast<uint16_t*>(w.scales)[e] = there ? scales[n * given + g] : 0;
+        if (w.has_zeros) const_cast<uint8_t*>(w.zeros)[e] = there ? zeros[n * given + g] & 15 : 0;
+    }
+}
+
+}  // namespace
+
+hipError_t launch_int4_pack(const uint8_t* codes, const void* scales, const uint8_t* zeros, const Int4Weights& w, uint8_t* blob, hipStream_t s) {
+    const long long words = (long long)w.output_tiles * w.input_tiles * (kTileBytes / 4);
+    const long long total = words + (long long)w.output_tiles * w.groups * kTileOutputs;
+    int4_pack_kernel<<<(unsigned)((total + 255) / 256), 256, 0, s>>>(codes, static_cast<const uint16_t*>(scales), zeros, w, blob, words, total);
+    return hipGetLastError();
+}
+
+}  // namespace wq
+
+using namespace wq;
+
+extern "C" {
+
+size_t int4_packed_bytes(int N, int K, int group, int has_zeros) {
+    return valid_weights(N, K, group) && !too_large(N, K) ? int4_layout(N, K, group, has_zeros != 0).total : 0;
+}
+
+int int4_pack_weights(const uint8_t* codes_dev, const void* scales_dev, int scale_type, const uint8_t* zeros_dev, int N, int K,
+                      int group, void* packed_dev, size_t packed_bytes, void* hip_stream) {
+    if (!codes_dev || !scales_dev || !packed_dev || !is_half(scale_type) || !valid_weights(N, K, group)) return WG_EINVAL;
+    if (!aligned(scales_dev, 2) || !aligned(packed_dev, 256)) return WG_EINVAL;
+    if (too_large(N, K)) return WG_EUNSUPPORTED;
+    const Int4Weights w = weights_of(packed_dev, N, K, group, scale_type, zeros_dev != nullptr);
+    if (packed_bytes < int4_packed_bytes(N, K, group, zeros_dev != nullptr)) return WG_ESMALLBUF;
+    return status_of(launch_int4_pack(codes_dev, scales_dev, zeros_dev, w, static_cast<uint8_t*>(packed_dev), static_cast<hipStream_t>(hip_stream)));
+}
+
+int int4_linear(const void* x_dev, int x_type, long long x_stride, const float* x_scale_dev, const void* packed_dev,
+                const float* bias_dev, void* y_dev, int y_type, int M, int N, int K, int group, int scale_type, int has_zeros,
+                int relu, void* hip_stream) {
+    if (!packed_dev || !valid_weights(N, K, group) || !is_half(scale_type)) return WG_EINVAL;
+    if (!(is_half(x_type) || x_type == WQ_I8) || !(is_half(y_type) || y_type == WQ_F32)) return WG_EINVAL;
+    if (x_scale_dev && x_type != WQ_I8) return WG_EINVAL;
+    if (M < 0 || x_stride < K) return WG_EINVAL;
+    if (M == 0) return WG_OK;
+    if (!x_dev || !y_dev) return WG_EINVAL;
+    if (!aligned(packed_dev, 256) || !aligned(y_dev, y_type == WQ_F32 ? 4 : 2) || !aligned(x_dev, x_type == WQ_I8 ? 1 : 2)) return WG_EINVAL;
+    if (!aligned(x_scale_dev, 4) || !aligned(bias_dev, 4)) return WG_EINVAL;
+    if (too_large(N, K)) return WG_EUNSUPPORTED;
+    const Int4Weights w = weights_of(packed_dev, N, K, group, scale_type, has_zeros != 0);
+    const Int4Output o = {x_scale_dev, bias_dev, y_dev, y_type, M, N, relu != 0};
+    return status_of(launch_int4_rows(x_dev, x_type, x_stride, w, o, static_cast<hipStream_t>(hip_stream)));
+}
+
+}  // extern "C"

@@ -1,0 +1,131 @@
+// y = x W^T with 4-bit weights for few rows: the weights' bytes are read once, everything else stays beside them.
+//
+// A workgroup takes 16 NT outputs and 16 MT rows; its waves share the inputs out by tiles of 128 and add their sums up in LDS at the
+// end, in the order of the waves.  The matrix cores multiply (rows beyond the last are copies of it and are not stored): a word of
+// eight codes costs seven vector instructions as float16 and three as int8 (int4_weights.h), the sum over a group of sum_k x_k that
+// takes the zero points off is one more product, whose other operand is constant, and becomes the accumulator that the codes'
+// products start from.
+#include "int4_weights.h"
+
+namespace wq {
+
+namespace {
+
+constexpr int kMostWaves = 8;
+
+template <int XT, int GROUP, bool ZEROS, int MT, int NT>
+__global__ __launch_bounds__(64 * kMostWaves) void int4_rows_kernel(const typename Element<XT>::type* x, long long x_stride, Int4Weights w, Int4Output o) {
+    typedef Products<XT> P;
+    typedef std::conditional_t<XT == WQ_I8, v2u, v4u> Bits;
+    constexpr int kGroups = kTileInputs / GROUP, kSteps = GROUP / 32;   // groups in a tile, products in a group
+    __shared__ v4f sums[kMostWaves][NT * MT][64];
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int tile0 = blockIdx.x * NT, m0 = blockIdx.y * (16 * MT);
+    const bool fits = matches(w), bf16_scales = w.scale_type == WQ_BF16;
+
+    const typename Element<XT>::type* row[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) row[mt] = x + (long long)min(m0 + 16 * mt + (lane & 15), o.M - 1) * x_stride;
+    const v4u* codes[NT];
+    size_t scale_at[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const size_t tile = min(tile0 + nt, w.output_tiles - 1);
+        codes[nt] = reinterpret_cast<const v4u*>(w.codes + tile * w.input_tiles * kTileBytes) + lane;
+        scale_at[nt] = tile * w.groups * kTileOutputs + 4 * (lane >> 4);
+    }
+
+    v4f acc[NT][MT] = {};
+    const typename P::Fragment ones = P::ones(ZEROS);
+    for (int kt = wave; kt < w.input_tiles; kt += waves) {
+        v4u words[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) words[nt] = codes[nt][(size_t)kt * (kTileBytes / 16)];
+        const bool whole = (kt + 1) * kTileInputs <= w.K;
+        typename P::Fragment xs[4][MT];
+#pragma unroll
+        for (int step = 0; step < 4; ++step)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+                xs[step][mt] = P::activations((Bits)load_inputs<XT>(row[mt], kt * kTileInputs + 32 * step + 8 * (lane >> 4), w.K, whole));
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            const size_t group = (size_t)(kt * kGroups + g) * kTileOutputs;
+            typename P::Sum off[MT];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                off[mt] = typename P::Sum{};
+#pragma unroll
+                for (int j = 0; j < kSteps; ++j) off[mt] = P::multiply(ones, xs[g * kSteps + j][mt], off[mt]);
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                typename P::Fragment ws[kSteps];
+#pragma unroll
+                for (int j = 0; j < kSteps; ++j) ws[j] = P::weights(words[nt][g * kSteps + j]);
+                const v4f scale = load_scales<XT>(w.scales + scale_at[nt] + group, bf16_scales);
+                uint32_t zeros = 0;
+                if (ZEROS) zeros = *reinterpret_cast<const uint32_t*>(w.zeros + scale_at[nt] + group);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    typename P::Sum sum = off[mt];
+                    if (ZEROS)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sum[i] = P::times_zero(off[mt][i], (int)(zeros >> (8 * i) & 255));
+#pragma unroll
+                    for (int j = 0; j < kSteps; ++j) sum = P::multiply(ws[j], xs[g * kSteps + j][mt], sum);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[nt][mt][i] = __builtin_fmaf((float)sum[i], scale[i], acc[nt][mt][i]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) sums[wave][nt * MT + mt][lane] = acc[nt][mt];
+    __syncthreads();
+    if (!fits) return;
+    for (int e = threadIdx.x; e < NT * MT * 64; e += blockDim.x) {
+        const int tile = e >> 6, l = e & 63;
+        v4f total = sums[0][tile][l];
+        for (int v = 1; v < waves; ++v) total += sums[v][tile][l];
+        store_outputs(o, m0 + 16 * (tile % MT) + (l & 15), (tile0 + tile / MT) * kTileOutputs + 4 * (l >> 4), total);
+    }
+}
+
+template <int XT, int GROUP, bool ZEROS, int MT, int NT>
+hipError_t launch(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
+    const dim3 grid(ceil_div(w.output_tiles, NT), ceil_div(o.M, 16 * MT));
+    if (grid.y > 65535) return hipErrorInvalidValue;
+    const int waves = min(kMostWaves, w.input_tiles);
+    int4_rows_kernel<XT, GROUP, ZEROS, MT, NT><<<grid, 64 * waves, 0, s>>>(static_cast<const typename Element<XT>::type*>(x), x_stride, w, o);
+    return hipGetLastError();
+}
+
+template <int XT, int GROUP, bool ZEROS>
+hipError_t launch_rows(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
+    if (o.M <= 16) return launch<XT, GROUP, ZEROS, 1, 1>(x, x_stride, w, o, s);
+    return launch<XT, GROUP, ZEROS, 4, 1>(x, x_stride, w, o, s);
+}
+
+template <int XT, int GROUP>
+hipError_t launch_zeros(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
+    return w.has_zeros ? launch_rows<XT, GROUP, true>(x, x_stride, w, o, s) : launch_rows<XT, GROUP, false>(x, x_stride, w, o, s);
+}
+
+template <int XT>
+hipError_t launch_group(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
+    return w.group == 32 ? launch_zeros<XT, 32>(x, x_stride, w, o, s)
+         : w.group == 64 ? launch_zeros<XT, 64>(x, x_stride, w, o, s) : launch_zeros<XT, 128>(x, x_stride, w, o, s);
+}
+
+}  // namespace
+
+hipError_t launch_int4_rows(const void* x, int x_type, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
+    return x_type == WQ_F16 ? launch_group<WQ_F16>(x, x_stride, w, o, s)
+         : x_type == WQ_BF16 ? launch_group<WQ_BF16>(x, x_stride, w, o, s) : launch_group<WQ_I8>(x, x_stride, w, o, s);
+}
+
+}  // namespace wq

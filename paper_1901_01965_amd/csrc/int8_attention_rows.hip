@@ -1,0 +1,356 @@
+// Attention over the cache held in 8 bits, for few rows per sequence: single tokens, and some guessed ahead.
+//
+// A workgroup takes 16 rows that read the same head of keys (the heads of a group, times a few tokens) and a part of the sequence's
+// tokens; its four waves take 64 tokens in turn and join at the end, parts of a sequence join in a second kernel.  One pass: running
+// largest score and sum per row.  The cache's bytes bound it, so a wave's loads are whole: 16 bytes a lane, of keys along head_dim, of
+// values along the tokens, and the next 64 tokens are on their way while these are worked on.
+//
+// Both products run on the matrix cores with codes turned into float16, exactly.  Scores are formed as K Q^T: in the 16x16 result a
+// lane holds one row's scores, so that maxima, exponentials and sums need no other lane but for the last step over four lanes.  Keys
+// enter the product in an order (row r of part t is token 16 (r / 4) + 4 t + r % 4) that leaves a lane with 16 neighbouring tokens'
+// scores, which is what it has to contribute to V^T P^T: they go from one product to the other inside the lane's registers.
+//
+// Scales: a key's is multiplied into its score.  A value's enters the weights, divided by the largest seen so far (what is summed is
+// brought in line when that grows), which keeps the weights within float16 at any ratio of the scales.
+#include "int8_attention.h"
+
+namespace wq {
+
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kStep = 64;        // tokens a wave takes at a time
+constexpr int kLeastSteps = 4;   // of a part of a sequence: one for each wave
+
+// A tile's rows and tokens.
+struct Tile {
+    Sequence sequence;
+    int s, token0, tokens;      // its first row in the sequence, rows
+    int head0, heads;           // first head of queries, heads
+    int begin, steps, per;      // tokens from `begin` on in steps of kStep, of which a part has `per`
+    int low, high;              // tokens that any row sees
+    int low_all, high_all;      // tokens that every row sees, unless low_all >= high_all
+};
+
+__device__ inline bool tile_of(const AttentionArgs& a, int tokens_shift, int head_tiles, int item, int y, Tile& t) {
+    const Batch& b = a.batch;
+    t.s = b.starts ? sequence_of_item(b, item, tokens_shift, 1) : item;
+    t.sequence = sequence_of(b, t.s);
+    t.token0 = b.starts ? (item - item_base(b, t.s, tokens_shift, 1)) << tokens_shift : 0;
+    if (t.token0 < 0 || t.token0 >= t.sequence.count) return false;
+    t.tokens = min(1 << tokens_shift, t.sequence.count - t.token0);
+    const int tile = y % head_tiles;
+    t.head0 = y / head_tiles * a.group + 16 * tile;
+    t.heads = min(a.group - 16 * tile, 16);
+    const int position = t.sequence.length - t.sequence.count + t.token0;
+    visible(a, position, t.sequence.length, t.low, t.high_all);
+    visible(a, position + t.tokens - 1, t.sequence.length, t.low_all, t.high);
+    t.begin = t.low & ~(kStep - 1);
+    t.steps = max(ceil_div(t.high - t.begin, kStep), 0);
+    t.per = ceil_div(t.steps, min(a.splits, max(t.steps / kLeastSteps, 1)));
+    return true;
+}
+
+template <int D>
+struct Loads {
+    v4u k[4][D / 64];
+    v4u v[D / 16];
+    float k_scale, v_scale;
+    int bad;   // the lane's 16 tokens lie in no block
+};
+
+template <int TYPE, int D>
+__global__ __launch_bounds__(64 * kWaves) void int8_attention_kernel(AttentionArgs a, int tokens_shift, int head_tiles) {
+    typedef typename Element<TYPE>::type T;
+    constexpr int kDims = D / 16;   // 16-row tiles of the result
+    constexpr int kRound = kDims < 8 ? kDims : 8;   // of which the waves join at a time
+    __shared__ v4f joined[kWaves][kRound][64];
+    __shared__ float row_largest[kWaves][16], row_sum[kWaves][16];
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int split = blockIdx.x % a.splits;
+    Tile t;
+    if (!tile_of(a, tokens_shift, head_tiles, blockIdx.x / a.splits, blockIdx.y, t)) return;
+    const int first_step = split * t.per, last_step = min(t.steps, first_step + t.per);
+    if (split > 0 && first_step >= t.steps) return;
+    const bool alone = t.per >= t.steps;
+
+    // the lane's row: for the scores' product its column, and again in the result
+    const int row = lane & 15, quarter = lane >> 4;
+    const bool real = row < t.tokens * t.heads;
+    const int row_token = real ? row / t.heads : 0, row_head = t.head0 + (real ? row % t.heads : 0);
+    const int position = t.sequence.length - t.sequence.count + t.token0 + row_token;
+    const long long row_at = (long long)(t.sequence.first + t.token0 + row_token);
+    int low, high;
+    visible(a, position, t.sequence.length, low, high);
+
+    const T* const query = static_cast<const T*>(a.q) + row_at * a.q_stride + (long long)row_head * D + 16 * quarter;
+    typedef T V8 __attribute__((ext_vector_type(8)));
+    V8 raw[D / 32];
+    float most = 0.0f;
+#pragma unroll
+    for (int f = 0; f < D / 32; ++f) {
+        raw[f] = load_unaligned<V8, 2>(query + 64 * (f >> 1) + 8 * (f & 1));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf((float)raw[f][j]));
+    }
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    float up, down;
+    query_powers<TYPE>(most, up, down);
+    v8h qs[D / 32];
+#pragma unroll
+    for (int f = 0; f < D / 32; ++f)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) qs[f][j] = (_Float16)((float)raw[f][j] * up);
+    const float to_exponent = a.scale_log2 * down;
+
+    const Batch& b = a.batch;
+    const int32_t* const table = b.table + (long long)t.s * b.width;
+    const int kv_head = blockIdx.y / head_tiles, block_mask = (1 << b.shift) - 1, last_block = (t.sequence.length - 1) >> b.shift;
+    const long long block_bytes = (long long)D << b.shift;
+
+    auto load = [&](Loads<D>& l, int step) {
+        const int token0 = t.begin + step * kStep;
+        const int of_k = token0 + 16 * (row >> 2), of_v = token0 + 16 * quarter;
+        int page_k = table[min(of_k >> b.shift, last_block)], page_v = table[min(of_v >> b.shift, last_block)];
+        l.bad = (unsigned)page_v >= (unsigned)b.blocks;
+        if ((unsigned)page_k >= (unsigned)b.blocks) page_k = 0;
+        if (l.bad) page_v = 0;
+        const long long at_v = (long long)page_v * a.kv_heads + kv_head;
+        const int8_t* const k = a.k + ((long long)page_k * a.kv_heads + kv_head) * block_bytes + ((of_k & block_mask) + (row & 3)) * D + 16 * quarter;
+#pragma unroll
+        for (int part = 0; part < 4; ++part)
+#pragma unroll
+            for (int f = 0; f < D / 64; ++f) l.k[part][f] = *reinterpret_cast<const v4u*>(k + 4 * part * D + 64 * f);
+        const int8_t* const v = a.v + at_v * block_bytes + (row << b.shift) + (of_v & block_mask);
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) l.v[d] = *reinterpret_cast<const v4u*>(v + (d << (b.shift + 4)));
+        l.k_scale = a.k_scale[at_v];
+        l.v_scale = a.v_scale[at_v];
+    };
+
+    v4f out[kDims] = {};
+    float largest = -INFINITY, lowered = 0.0f, sum = 0.0f, unit = 0.0f;   // unit: the scale in which `out` is held
+    int step = first_step + wave;
+    Loads<D> next;
+    if (step < last_step) load(next, step);
+    for (; step < last_step; step += kWaves) {
+        const Loads<D> now = next;
+        if (step + kWaves < last_step) load(next, step + kWaves);
+
+        float k_scale = now.k_scale, v_scale = now.v_scale;
+        const int token0 = t.begin + step * kStep + 16 * quarter;   // the first of the lane's tokens
+        const bool masked = t.begin + step * kStep < t.low_all || t.begin + (step + 1) * kStep > t.high_all || __any(now.bad);
+        v4f scores[4];
+#pragma unroll
+        for (int part = 0; part < 4; ++part) {
+            scores[part] = v4f{};
+#pragma unroll
+            for (int f = 0; f < D / 64; ++f) {
+                scores[part] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half(now.k[part][f][0], now.k[part][f][1]), qs[2 * f], scores[part], 0, 0, 0);
+                scores[part] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half(now.k[part][f][2], now.k[part][f][3]), qs[2 * f + 1], scores[part], 0, 0, 0);
+            }
+        }
+        const float factor = k_scale * to_exponent;
+        float top = -INFINITY;
+#pragma unroll
+        for (int part = 0; part < 4; ++part)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) scores[part][i] *= factor;
+        if (masked) {
+            // scales of blocks that no row sees are whatever lies there
+            if (now.bad || token0 >= t.high || token0 + 16 <= t.low) v_scale = 0.0f;
+#pragma unroll
+            for (int part = 0; part < 4; ++part)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int token = token0 + 4 * part + i;
+                    if (now.bad || token < low || token >= high) scores[part][i] = -INFINITY;
+                }
+        }
+#pragma unroll
+        for (int part = 0; part < 4; ++part)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, scores[part][i]);
+        if (__any(top > largest + kSlack || v_scale > unit)) {
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            float scale = fmaxf(v_scale, __shfl_xor(v_scale, 16));
+            scale = fmaxf(unit, fmaxf(scale, __shfl_xor(scale, 32)));
+            const float now_largest = fmaxf(largest, top);
+            const float change = now_largest == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(largest - now_largest);
+            sum *= change;
+            const float rescale = scale > 0.0f ? change * (unit / scale) : 0.0f;
+#pragma unroll
+            for (int d = 0; d < kDims; ++d) out[d] *= rescale;
+            largest = now_largest;
+            lowered = now_largest == -INFINITY ? 0.0f : now_largest - kRaise;
+            unit = scale;
+        }
+        const float ratio = unit > 0.0f ? v_scale / unit : 0.0f;
+        v8h weights[2];
+#pragma unroll
+        for (int part = 0; part < 4; ++part)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float p = __builtin_amdgcn_exp2f(scores[part][i] - lowered);
+                sum += p;
+                weights[part >> 1][4 * (part & 1) + i] = (_Float16)(p * ratio);
+            }
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) {
+            out[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half(now.v[d][0], now.v[d][1]), weights[0], out[d], 0, 0, 0);
+            out[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half(now.v[d][2], now.v[d][3]), weights[1], out[d], 0, 0, 0);
+        }
+    }
+
+    // join the waves: every one's sums come to the largest score of all
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (lane < 16) {
+        row_largest[wave][row] = largest;
+        row_sum[wave][row] = sum;
+    }
+    __syncthreads();
+    float all = row_largest[0][row];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) all = fmaxf(all, row_largest[w][row]);
+    float total = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+        if (row_largest[w][row] != -INFINITY) total += row_sum[w][row] * __builtin_amdgcn_exp2f(row_largest[w][row] - all);
+    const float mine = largest == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(largest - all) * unit;
+    const float over = total == 0.0f ? 0.0f : 1.0f / total;   // NaN stays NaN
+    float* const partial = a.partial + (((long long)(blockIdx.x / a.splits) * gridDim.y + blockIdx.y) * a.splits + split) * (16 * (D + 2));
+    if (!alone && threadIdx.x < 16) {
+        partial[16 * D + 2 * row] = all;
+        partial[16 * D + 2 * row + 1] = total;
+    }
+#pragma unroll
+    for (int first = 0; first < kDims; first += kRound) {
+        if (first > 0) __syncthreads();
+#pragma unroll
+        for (int d = 0; d < kRound; ++d) joined[wave][d][lane] = out[first + d] * mine;
+        __syncthreads();
+        for (int e = wave; e < kRound; e += kWaves) {
+            v4f r = joined[0][e][lane];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) r += joined[w][e][lane];
+            const int d = 16 * (first + e) + 4 * quarter;
+            if (!real) continue;
+            if (alone) store4<TYPE>(a.out, row_at * a.out_stride + (long long)row_head * D + d, r * over);
+            else *reinterpret_cast<v4f*>(partial + row * D + d) = r;
+        }
+    }
+}
+
+// Joins the parts of a row: one workgroup per row, its threads share the parts out.
+template <int TYPE, int D>
+__global__ __launch_bounds__(256) void int8_attention_join_kernel(AttentionArgs a, int tokens_shift, int head_tiles) {
+    constexpr int kAcross = D / 4, kDown = 256 / kAcross;
+    __shared__ v4f sums[kDown][kAcross];
+    __shared__ float totals[kDown];
+    Tile t;
+    if (!tile_of(a, tokens_shift, head_tiles, blockIdx.x / 16, blockIdx.y, t)) return;
+    const int row = blockIdx.x & 15;
+    if (row >= t.tokens * t.heads || t.per >= t.steps) return;
+    const int parts = ceil_div(t.steps, t.per), across = threadIdx.x % kAcross, down = threadIdx.x / kAcross;
+    const long long each = 16 * (D + 2);
+    const float* const partial = a.partial + ((long long)(blockIdx.x / 16) * gridDim.y + blockIdx.y) * a.splits * each;
+    float all = -INFINITY;
+    for (int p = 0; p < parts; ++p) all = fmaxf(all, partial[p * each + 16 * D + 2 * row]);
+    v4f r = {};
+    float total = 0.0f;
+    for (int p = down; p < parts; p += kDown) {
+        const float* const part = partial + p * each;
+        const float largest = part[16 * D + 2 * row];
+        const float factor = largest == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(largest - all);
+        if (largest != -INFINITY) total += part[16 * D + 2 * row + 1] * factor;
+        r += *reinterpret_cast<const v4f*>(part + row * D + 4 * across) * factor;
+    }
+    sums[down][across] = r;
+    if (across == 0) totals[down] = total;
+    __syncthreads();
+    if (down != 0) return;
+    for (int i = 1; i < kDown; ++i) {
+        r += sums[i][across];
+        total += totals[i];
+    }
+    const float over = total == 0.0f ? 0.0f : 1.0f / total;
+    const long long row_at = (long long)(t.sequence.first + t.token0 + row / t.heads);
+    store4<TYPE>(a.out, row_at * a.out_stride + (long long)(t.head0 + row % t.heads) * D + 4 * across, r * over);
+}
+
+template <int TYPE, int D>
+hipError_t launch(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) {
+    const unsigned y = a.kv_heads * p.head_tiles;
+    int8_attention_kernel<TYPE, D><<<dim3((unsigned)(p.items * p.splits), y), 64 * kWaves, 0, s>>>(a, p.tokens_shift, p.head_tiles);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (p.splits > 1) int8_attention_join_kernel<TYPE, D><<<dim3((unsigned)(p.items * 16), y), 256, 0, s>>>(a, p.tokens_shift, p.head_tiles);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+AttentionPlan plan_attention(int rows, int heads, int kv_heads, int head_dim, int block, int width, int sequences, bool has_starts) {
+    AttentionPlan p;
+    const int group = heads / kv_heads;
+    p.head_tiles = ceil_div(group, 16);
+    p.tokens_shift = 0;
+    while (has_starts && (2 << p.tokens_shift) * group <= 16) ++p.tokens_shift;
+    p.items = has_starts ? item_count(rows, sequences, p.tokens_shift, 1) : sequences;
+    const long long tiles = p.items * kv_heads * p.head_tiles;
+    const long long most = max((long long)width * block / (kStep * kLeastSteps), 1ll);
+    p.splits = (int)min(max((8ll * kComputeUnits + tiles - 1) / tiles, 1ll), most);
+    p.workspace = p.splits > 1 ? (size_t)tiles * p.splits * 16 * (head_dim + 2) * sizeof(float) : 0;
+    return p;
+}
+
+hipError_t launch_attention_rows(const AttentionArgs& a, const AttentionPlan& p, int type, int head_dim, hipStream_t s) {
+    if (type == WQ_F16) return head_dim == 64 ? launch<WQ_F16, 64>(a, p, s) : head_dim == 128 ? launch<WQ_F16, 128>(a, p, s) : launch<WQ_F16, 256>(a, p, s);
+    return head_dim == 64 ? launch<WQ_BF16, 64>(a, p, s) : head_dim == 128 ? launch<WQ_BF16, 128>(a, p, s) : launch<WQ_BF16, 256>(a, p, s);
+}
+
+}  // namespace wq
+
+using namespace wq;
+
+extern "C" {
+
+size_t int8_cache_attention_workspace_bytes(int rows, int heads, int kv_heads, int head_dim, int block, int table_width,
+                                            int sequences, int has_starts) {
+    if (rows <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || table_width <= 0 || sequences <= 0) return 0;
+    if ((head_dim != 64 && head_dim != 128 && head_dim != 256) || (block != 16 && block != 32 && block != 64 && block != 128)) return 0;
+    return plan_attention(rows, heads, kv_heads, head_dim, block, table_width, sequences, has_starts != 0).workspace;
+}
+
+int int8_cache_attention(const void* q_dev, long long q_stride, int type, int rows, int heads, const int8_t* cache_k_dev,
+                         const int8_t* cache_v_dev, const float* k_scale_dev, const float* v_scale_dev, int blocks, int kv_heads,
+                         int head_dim, int block, const int32_t* table_dev, int table_width, int sequences,
+                         const int32_t* lengths_dev, const int32_t* starts_dev, float scale, int causal, int window, void* out_dev,
+                         long long out_stride, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+    const CacheArgs c = {cache_k_dev, cache_v_dev, k_scale_dev, v_scale_dev, blocks, kv_heads, head_dim, block};
+    if (int st = check_cache(c)) return st;
+    bool empty;
+    if (int st = check_batch(rows, table_dev, table_width, sequences, lengths_dev, starts_dev, block, empty)) return st;
+    if (!is_half(type) || heads <= 0 || heads % kv_heads || window < 0 || (window > 0 && !causal)) return WG_EINVAL;
+    if (!(scale - scale == 0.0f)) return WG_EINVAL;   // infinite or NaN
+    if (heads > 8192) return WG_EUNSUPPORTED;
+    if (q_stride < (long long)heads * head_dim || out_stride < (long long)heads * head_dim) return WG_EINVAL;
+    if (empty) return WG_OK;
+    if (!q_dev || !out_dev || !aligned(q_dev, 2) || !aligned(out_dev, 2)) return WG_EINVAL;
+    const AttentionPlan p = plan_attention(rows, heads, kv_heads, head_dim, block, table_width, sequences, starts_dev != nullptr);
+    if (p.items * max(p.splits, 16) > kMostItems) return WG_EUNSUPPORTED;
+    if (p.workspace > 0) {
+        if (!workspace_dev || !aligned(workspace_dev, 256)) return WG_EINVAL;
+        if (workspace_bytes < p.workspace) return WG_ESMALLBUF;
+    }
+    const AttentionArgs a = {q_dev, q_stride, out_dev, out_stride, cache_k_dev, cache_v_dev, k_scale_dev, v_scale_dev,
+                             static_cast<float*>(workspace_dev),
+                             {table_dev, lengths_dev, starts_dev, table_width, sequences, rows, blocks, block_shift(block)},
+                             kv_heads, heads / kv_heads, causal != 0, window, p.splits, scale * 1.44269504088896340736f};
+    return status_of(launch_attention_rows(a, p, type, head_dim, static_cast<hipStream_t>(hip_stream)));
+}
+
+}  // extern "C"

@@ -1,0 +1,38 @@
+// Checks that the entry points of the 8-bit cache share.
+#pragma once
+#include "quantized_common.h"
+
+namespace wq {
+
+constexpr int kMostItems = 1 << 23;   // workgroups along a grid's first dimension: 2^31 threads of 256
+
+struct CacheArgs {
+    const int8_t *k, *v;
+    const float *k_scale, *v_scale;
+    int blocks, kv_heads, head_dim, block;
+};
+
+inline int block_shift(int block) { return block == 16 ? 4 : block == 32 ? 5 : block == 64 ? 6 : 7; }
+
+inline int check_cache(const CacheArgs& c) {
+    if (!c.k || !c.v || !c.k_scale || !c.v_scale || c.blocks <= 0 || c.kv_heads <= 0) return WG_EINVAL;
+    if (!aligned(c.k, 16) || !aligned(c.v, 16) || !aligned(c.k_scale, 16) || !aligned(c.v_scale, 16)) return WG_EINVAL;
+    if (c.head_dim != 64 && c.head_dim != 128 && c.head_dim != 256) return WG_EUNSUPPORTED;
+    if (c.block != 16 && c.block != 32 && c.block != 64 && c.block != 128) return WG_EUNSUPPORTED;
+    if (c.kv_heads > 1024) return WG_EUNSUPPORTED;
+    return WG_OK;
+}
+
+// Nothing to do (no rows, or no sequences for them to belong to) is no error: `empty`.
+inline int check_batch(int rows, const int32_t* table, int width, int sequences, const int32_t* lengths, const int32_t* starts, int block,
+                       bool& empty) {
+    empty = rows == 0 || sequences == 0;
+    if (rows < 0 || sequences < 0 || (!starts && rows != sequences)) return WG_EINVAL;
+    if (empty) return WG_OK;
+    if (width <= 0 || !table || !lengths) return WG_EINVAL;
+    if (!aligned(table, 4) || !aligned(lengths, 4) || !aligned(starts, 4)) return WG_EINVAL;
+    if ((long long)width * block > 0x7fffff00ll) return WG_EUNSUPPORTED;   // positions are ints
+    return WG_OK;
+}
+
+}  // namespace wq

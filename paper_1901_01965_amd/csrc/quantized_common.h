@@ -1,0 +1,86 @@
+// Pieces shared by the quantised operators beside the convolutions (int4_*.hip, int8_cache*.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "quantized_c.h"
+
+namespace wq {
+
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef _Float16 v4h __attribute__((ext_vector_type(4)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef uint16_t v8s __attribute__((ext_vector_type(8)));
+
+// A value of T wherever it lies, read with one load where the element type's alignment is all that is known.
+template <class T, int ALIGN>
+__device__ inline T load_unaligned(const void* p) {
+    struct __attribute__((packed, aligned(ALIGN))) Box { T v; };
+    return static_cast<const Box*>(p)->v;
+}
+
+template <int ALIGN, class T>
+__device__ inline void store_unaligned(void* p, const T& v) {
+    struct __attribute__((packed, aligned(ALIGN))) Box { T v; };
+    static_cast<Box*>(p)->v = v;
+}
+
+template <int TYPE> struct Element;
+template <> struct Element<WQ_F16> { typedef _Float16 type; };
+template <> struct Element<WQ_BF16> { typedef __bf16 type; };
+template <> struct Element<WQ_I8> { typedef int8_t type; };
+template <> struct Element<WQ_F32> { typedef float type; };
+
+inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+inline int status_of(hipError_t e) { return e == hipSuccess ? WG_OK : WG_ERUNTIME; }
+inline bool is_half(int type) { return type == WQ_F16 || type == WQ_BF16; }
+__host__ __device__ inline int ceil_div(int a, int b) { return a / b + (a % b != 0); }
+
+// Compute units of an MI355X: what a launch has to fill.
+constexpr int kComputeUnits = 256;
+
+// ---- the cache's batch, as the kernels see it --------------------------------------------------------------------
+
+struct Batch {
+    const int32_t* table;
+    const int32_t* lengths;
+    const int32_t* starts;   // null: one row per sequence
+    int width, sequences, rows, blocks, shift;   // a block holds 1 << shift tokens
+};
+
+// Rows first .. first + count - 1 of the call are the last `count` of the sequence's `length` tokens.
+struct Sequence {
+    int first, count, length;
+};
+
+__device__ inline int start_of(const Batch& b, int s) {
+    return b.starts ? min(max(b.starts[s], 0), b.rows) : s;
+}
+
+__device__ inline Sequence sequence_of(const Batch& b, int s) {
+    const int first = start_of(b, s);
+    const int most = (int)min((long long)b.width << b.shift, 0x7fffffffll);
+    return {first, max(start_of(b, s + 1) - first, 0), min(max(b.lengths[s], 0), most)};
+}
+
+// Work items are dealt to sequences without a table of their sums: sequence s owns the items base(s) .. base(s + 1) - 1 with
+// base(s) = floor(start(s) / unit) + extra * s, which are at least count / unit, rounded up, plus extra - 1.  Finds the sequence of
+// an item; starts that fall are read as a clamped search finds them.
+__device__ inline int item_base(const Batch& b, int s, int unit_shift, int extra) { return (start_of(b, s) >> unit_shift) + extra * s; }
+__device__ inline int sequence_of_item(const Batch& b, int item, int unit_shift, int extra) {
+    int low = 0, high = b.sequences - 1;
+    while (low < high) {
+        const int middle = (low + high + 1) >> 1;
+        if (item_base(b, middle, unit_shift, extra) <= item) low = middle;
+        else high = middle - 1;
+    }
+    return low;
+}
+inline long long item_count(int rows, int sequences, int unit_shift, int extra) { return (rows >> unit_shift) + (long long)extra * sequences; }
+
+}  // namespace wq

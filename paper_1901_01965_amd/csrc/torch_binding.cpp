@@ -9,11 +9,13 @@
 #include <Python.h>
 
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "host_api.h"
+#include "quantized_c.h"
 
 namespace {
 
@@ -282,9 +284,261 @@ PyObject* requant_relu_pool(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- quantised operators of quantized_c.h ------------------------------------------------------------------------
+
+const char* element_name(at::ScalarType t) {
+    return t == at::kHalf ? "torch.float16" : t == at::kBFloat16 ? "torch.bfloat16" : t == at::kFloat ? "torch.float32" : type_name(t);
+}
+
+int element_type(at::ScalarType t) {
+    return t == at::kHalf ? WQ_F16 : t == at::kBFloat16 ? WQ_BF16 : t == at::kChar ? WQ_I8 : t == at::kFloat ? WQ_F32 : -1;
+}
+
+// The tensors of a call have to be on one device, and the kernels run on the current one.
+struct Device {
+    int index = -1;
+    const at::Tensor& tensor(PyObject* o, const char* what) {
+        if (THPVariable_Check(o)) {
+            const at::Tensor& t = THPVariable_Unpack(o);
+            if (t.is_cuda()) {
+                if (index < 0) index = t.device().index();
+                if (t.device().index() != index) {
+                    PyErr_Format(PyExc_ValueError, "%s is on another device", what);
+                    throw PyError();
+                }
+                if (t.requires_grad() && c10::GradMode::is_enabled()) {
+                    PyErr_Format(PyExc_RuntimeError, "%s requires a gradient: this call has no backward pass", what);
+                    throw PyError();
+                }
+                return t;
+            }
+        }
+        PyErr_Format(PyExc_TypeError, "%s must be a CUDA tensor", what);
+        throw PyError();
+    }
+    void need_current() const {
+        if (index != c10::hip::current_device()) fail(PyExc_ValueError, "the tensors are not on the current device");
+    }
+};
+
+// A dense tensor of this type and shape.
+const at::Tensor& dense(Device& on, PyObject* o, at::ScalarType dtype, at::IntArrayRef shape, const char* what) {
+    const at::Tensor& t = on.tensor(o, what);
+    if (t.scalar_type() != dtype || !t.is_contiguous()) {
+        PyErr_Format(PyExc_TypeError, "%s must be a contiguous CUDA tensor of %s", what, element_name(dtype));
+        throw PyError();
+    }
+    if (t.sizes() != shape) {
+        PyErr_Format(PyExc_ValueError, "%s does not have the shape that the other arguments give it", what);
+        throw PyError();
+    }
+    return t;
+}
+
+int small(int64_t n, const char* what) {
+    if (n > 0x7fffffff) {
+        PyErr_Format(PyExc_ValueError, "%s: dimension too large", what);
+        throw PyError();
+    }
+    return (int)n;
+}
+
+// Rows of dense elements, `row` elements each, that do not overlap: how far they lie apart.
+int64_t row_stride(const at::Tensor& t, int64_t row, const char* what) {
+    int64_t expected = 1;
+    bool fits = true;
+    for (int64_t i = t.dim() - 1; i > 0; --i) {
+        fits = fits && (t.size(i) == 1 || t.stride(i) == expected);
+        expected *= t.size(i);
+    }
+    if (t.size(0) <= 1 || t.numel() == 0) return fits || t.numel() == 0 ? row : (fail(PyExc_ValueError, "rows must be dense"), 0);
+    if (!fits || t.stride(0) < row) {
+        PyErr_Format(PyExc_ValueError, "%s must have dense rows that do not overlap", what);
+        throw PyError();
+    }
+    return t.stride(0);
+}
+
+// (x, blob, N, K, group, scale type, has zeros, bias or None, relu, x_scale or None, output type, out or None)
+PyObject* int4_linear_call(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 12, [&]() -> PyObject* {
+        const int N = integer(a[2]), K = integer(a[3]), group = integer(a[4]), scale_type = integer(a[5]), zeros = integer(a[6]);
+        const int relu = integer(a[8]), out_type = integer(a[10]);
+        Device on;
+        const at::Tensor& x = on.tensor(a[0], "x");
+        const int x_type = element_type(x.scalar_type());
+        if (x_type < 0 || x_type == WQ_F32) fail(PyExc_TypeError, "x must be a tensor of torch.float16, torch.bfloat16 or torch.int8");
+        if (x.dim() < 1 || x.size(x.dim() - 1) != K) {
+            PyErr_Format(PyExc_ValueError, "x does not have %d inputs in its last dimension, which the weights were packed for", K);
+            throw PyError();
+        }
+        if (x.dim() != 2 && !x.is_contiguous()) fail(PyExc_ValueError, "x of other than two dimensions must be contiguous");
+        const int M = small(x.numel() / K, "x");
+        const int64_t stride = x.dim() == 2 ? row_stride(x, K, "x") : K;
+        const void* const xp = data<void>(x);
+        const void* const blob = data<void>(dense(on, a[1], at::kByte, {(int64_t)int4_packed_bytes(N, K, group, zeros)}, "blob"));
+        const float* const bias = a[7] == Py_None ? nullptr : data<float>(dense(on, a[7], at::kFloat, {N}, "bias"));
+        if (a[9] != Py_None && x_type != WQ_I8) fail(PyExc_TypeError, "x_scale goes with x of torch.int8");
+        const float* const x_scale = a[9] == Py_None ? nullptr : data<float>(dense(on, a[9], at::kFloat, {M}, "x_scale"));
+        const at::ScalarType out_dtype = out_type == WQ_F16 ? at::kHalf : out_type == WQ_BF16 ? at::kBFloat16 : at::kFloat;
+        c10::DimVector shape(x.sizes().begin(), x.sizes().end());
+        shape.back() = N;
+        at::Tensor y;
+        if (a[11] != Py_None) y = dense(on, a[11], out_dtype, shape, "out");
+        on.need_current();
+        if (a[11] == Py_None) y = at::Tensor(at::detail::empty_cuda(shape, out_dtype, x.device(), std::nullopt));
+        void* const yp = data<void>(y);
+        void* const s = stream();
+        return finish(y, [&] {
+            return int4_linear(xp, x_type, stride, x_scale, blob, bias, yp, out_type, M, N, K, group, scale_type, zeros, relu, s);
+        });
+    });
+}
+
+struct Cache {
+    int8_t *k, *v;
+    float *k_scale, *v_scale;
+    int blocks, heads, dim, block;
+    Cache(Device& on, PyObject* k_, PyObject* v_, PyObject* k_scale_, PyObject* v_scale_) {
+        const at::Tensor& t = on.tensor(k_, "cache.k");
+        if (t.dim() != 4) fail(PyExc_ValueError, "cache.k has four dimensions");
+        blocks = small(t.size(0), "cache.k"); heads = small(t.size(1), "cache.k"); block = small(t.size(2), "cache.k"); dim = small(t.size(3), "cache.k");
+        k = data<int8_t>(dense(on, k_, at::kChar, {blocks, heads, block, dim}, "cache.k"));
+        v = data<int8_t>(dense(on, v_, at::kChar, {blocks, heads, dim, block}, "cache.v"));
+        k_scale = data<float>(dense(on, k_scale_, at::kFloat, {blocks, heads}, "cache.k_scale"));
+        v_scale = data<float>(dense(on, v_scale_, at::kFloat, {blocks, heads}, "cache.v_scale"));
+    }
+};
+
+struct BatchTensors {
+    const int32_t *table, *lengths, *starts;
+    int width, sequences;
+    BatchTensors(Device& on, PyObject* table_, PyObject* lengths_, PyObject* starts_) {
+        const at::Tensor& t = on.tensor(table_, "block_table");
+        if (t.dim() != 2) fail(PyExc_ValueError, "block_table has two dimensions");
+        sequences = small(t.size(0), "block_table");
+        width = small(t.size(1), "block_table");
+        table = data<int32_t>(dense(on, table_, at::kInt, {sequences, width}, "block_table"));
+        lengths = data<int32_t>(dense(on, lengths_, at::kInt, {sequences}, "lengths"));
+        starts = starts_ == Py_None ? nullptr : data<int32_t>(dense(on, starts_, at::kInt, {(int64_t)sequences + 1}, "starts"));
+    }
+    void need_rows(int rows, const char* what) const {
+        if (starts || rows == sequences) return;
+        PyErr_Format(PyExc_ValueError, "%s has %d rows for %d sequences; other than one row each needs starts", what, rows, sequences);
+        throw PyError();
+    }
+};
+
+// Rows of heads: a float16 or bfloat16 tensor [rows][heads][dim], the heads of a row dense.
+const at::Tensor& head_rows(Device& on, PyObject* o, int dim, const char* what) {
+    const at::Tensor& t = on.tensor(o, what);
+    if (t.scalar_type() != at::kHalf && t.scalar_type() != at::kBFloat16) {
+        PyErr_Format(PyExc_TypeError, "%s must be a tensor of torch.float16 or torch.bfloat16", what);
+        throw PyError();
+    }
+    if (t.dim() != 3 || t.size(2) != dim) {
+        PyErr_Format(PyExc_ValueError, "%s must have three dimensions, the last of the cache's %d", what, dim);
+        throw PyError();
+    }
+    return t;
+}
+
+// (k, v, cache k, v, k_scale, v_scale, table, lengths, starts or None)
+PyObject* int8_cache_append_call(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 9, [&]() -> PyObject* {
+        Device on;
+        const Cache c(on, a[2], a[3], a[4], a[5]);
+        const BatchTensors b(on, a[6], a[7], a[8]);
+        const at::Tensor &k = head_rows(on, a[0], c.dim, "k"), &v = head_rows(on, a[1], c.dim, "v");
+        if (k.size(1) != c.heads || v.sizes() != k.sizes() || v.scalar_type() != k.scalar_type())
+            fail(PyExc_ValueError, "k and v must have one type and shape, with the cache's heads");
+        const int rows = small(k.size(0), "k"), type = element_type(k.scalar_type());
+        b.need_rows(rows, "k");
+        const int64_t k_stride = row_stride(k, (int64_t)c.heads * c.dim, "k"), v_stride = row_stride(v, (int64_t)c.heads * c.dim, "v");
+        const void *const kp = data<void>(k), *const vp = data<void>(v);
+        on.need_current();
+        void* const s = stream();
+        int status;
+        {
+            const Unlocked unlocked;
+            status = int8_cache_append(kp, k_stride, vp, v_stride, type, rows, c.k, c.v, c.k_scale, c.v_scale, c.blocks, c.heads, c.dim,
+                                       c.block, b.table, b.width, b.sequences, b.lengths, b.starts, s);
+        }
+        return PyLong_FromLong(status);
+    });
+}
+
+// (cache k, v, k_scale, v_scale, ids, output type)
+PyObject* int8_cache_read_call(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 6, [&]() -> PyObject* {
+        Device on;
+        const Cache c(on, a[0], a[1], a[2], a[3]);
+        const at::Tensor& ids = on.tensor(a[4], "blocks");
+        const int count = small(ids.numel(), "blocks"), type = integer(a[5]);
+        const int32_t* const ip = data<int32_t>(dense(on, a[4], at::kInt, {count}, "blocks"));
+        on.need_current();
+        const at::ScalarType dtype = type == WQ_F16 ? at::kHalf : type == WQ_BF16 ? at::kBFloat16 : at::kFloat;
+        const int64_t shape[4] = {count, c.heads, c.block, c.dim};
+        const at::Tensor k = at::Tensor(at::detail::empty_cuda(at::IntArrayRef(shape, 4), dtype, ids.device(), std::nullopt));
+        const at::Tensor v = at::Tensor(at::detail::empty_cuda(at::IntArrayRef(shape, 4), dtype, ids.device(), std::nullopt));
+        void *const kp = data<void>(k), *const vp = data<void>(v), *const s = stream();
+        int status;
+        {
+            const Unlocked unlocked;
+            status = int8_cache_read(c.k, c.v, c.k_scale, c.v_scale, c.blocks, c.heads, c.dim, c.block, ip, count, kp, vp, type, s);
+        }
+        if (status != WG_OK) return PyLong_FromLong(status);
+        PyObject* const first = THPVariable_Wrap(k);
+        PyObject* const second = first ? THPVariable_Wrap(v) : nullptr;
+        PyObject* const pair = second ? PyTuple_Pack(2, first, second) : nullptr;
+        Py_XDECREF(first);
+        Py_XDECREF(second);
+        return pair;
+    });
+}
+
+// (q, cache k, v, k_scale, v_scale, table, lengths, starts or None, scale, causal, window, out or None)
+PyObject* int8_cache_attention_call(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 12, [&]() -> PyObject* {
+        Device on;
+        const Cache c(on, a[1], a[2], a[3], a[4]);
+        const BatchTensors b(on, a[5], a[6], a[7]);
+        const at::Tensor& q = head_rows(on, a[0], c.dim, "q");
+        const double scale = PyFloat_AsDouble(a[8]);
+        if (scale == -1.0 && PyErr_Occurred()) throw PyError();
+        const int causal = integer(a[9]), window = integer(a[10]);
+        const int rows = small(q.size(0), "q"), heads = small(q.size(1), "q"), type = element_type(q.scalar_type());
+        if (c.heads == 0 || heads == 0 || heads % c.heads != 0) fail(PyExc_ValueError, "the heads of q must be a multiple of the cache's");
+        b.need_rows(rows, "q");
+        const int64_t row = (int64_t)heads * c.dim, q_stride = row_stride(q, row, "q");
+        const void* const qp = data<void>(q);
+        at::Tensor out;
+        int64_t out_stride = row;
+        if (a[11] == Py_None) {
+            on.need_current();
+            out = at::Tensor(at::detail::empty_cuda(q.sizes(), q.scalar_type(), q.device(), std::nullopt));
+        } else {
+            out = head_rows(on, a[11], c.dim, "out");
+            if (out.scalar_type() != q.scalar_type() || out.sizes() != q.sizes()) fail(PyExc_ValueError, "out must have the type and shape of q");
+            out_stride = row_stride(out, row, "out");
+            on.need_current();
+        }
+        void* const op = data<void>(out);
+        void* const s = stream();
+        const ScratchTensor scratch(
+            int8_cache_attention_workspace_bytes(rows, heads, c.heads, c.dim, c.block, b.width, b.sequences, b.starts != nullptr), q, true);
+        return finish(out, [&] {
+            return int8_cache_attention(qp, q_stride, type, rows, heads, c.k, c.v, c.k_scale, c.v_scale, c.blocks, c.heads, c.dim, c.block,
+                                        b.table, b.width, b.sequences, b.lengths, b.starts, (float)scale, causal, window, op, out_stride,
+                                        scratch.p, scratch.bytes, s);
+        });
+    });
+}
+
 #define WG_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {WG_METHOD(conv2d_int8),   WG_METHOD(conv2d_int8_requant), WG_METHOD(conv2d_bytes), WG_METHOD(conv2d_act_scaled),
-                         WG_METHOD(direct_conv2d), WG_METHOD(requant_relu_pool),   {nullptr, nullptr, 0, nullptr}};
+                         WG_METHOD(direct_conv2d), WG_METHOD(requant_relu_pool), WG_METHOD(int4_linear_call), WG_METHOD(int8_cache_append_call),
+                         WG_METHOD(int8_cache_read_call), WG_METHOD(int8_cache_attention_call), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_winograd_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,187 @@
+"""Quantised operators beside the convolutions: products with 4-bit weights, and a cache of attention keys and values held
+in 8 bits with the attention that reads it.
+
+Thin binding of include/quantized_c.h, in the manner of ``binding``: every step runs in the library's HIP kernels on the current
+device and stream, outputs and scratch memory come from torch's caching allocator, and a call that is refused raises
+TypeError, ValueError or WinogradError before anything is enqueued.  These calls have no backward pass and refuse tensors
+that ask for a gradient.  All of them can be captured into a graph.
+"""
+import ctypes
+import math
+
+import torch
+
+from .binding import WinogradError, _check, _done, _native, _need, _ptr, _stream, load_library
+
+F16, BF16, I8, F32 = 0, 1, 2, 3
+_TYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
+
+EXPORTED_SYMBOLS = ("int4_packed_bytes", "int4_pack_weights", "int4_linear", "int8_cache_append", "int8_cache_read",
+                    "int8_cache_attention_workspace_bytes", "int8_cache_attention")
+
+_ready = None
+
+
+def load_quantized():
+    """The library with the signatures of include/quantized_c.h."""
+    global _ready
+    if _ready is None:
+        lib = load_library()
+        vp, i, sz, ll, f = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_longlong, ctypes.c_float
+        cache, batch = [vp] * 4 + [i] * 4, [vp, i, i, vp, vp]
+        sigs = {
+            "int4_packed_bytes": (sz, [i] * 4),
+            "int4_pack_weights": (i, [vp, vp, i, vp, i, i, i, vp, sz, vp]),
+            "int4_linear": (i, [vp, i, ll, vp, vp, vp, vp] + [i] * 8 + [vp]),
+            "int8_cache_append": (i, [vp, ll, vp, ll, i, i] + cache + batch + [vp]),
+            "int8_cache_read": (i, cache + [vp, i, vp, vp, i, vp]),
+            "int8_cache_attention_workspace_bytes": (sz, [i] * 8),
+            "int8_cache_attention": (i, [vp, ll, i, i, i] + cache + batch + [f, i, i, vp, ll, vp, sz, vp]),
+        }
+        for name, (res, args) in sigs.items():
+            fn = getattr(lib, name)
+            fn.restype, fn.argtypes = res, args
+        _ready = lib
+    return _ready
+
+
+def _out_type(dtype, what):
+    if dtype not in _TYPES:
+        raise TypeError("%s must be torch.float16, torch.bfloat16 or torch.float32" % what)
+    return _TYPES[dtype]
+
+
+# ---- products with 4-bit weights ------------------------------------------------------------------------------
+
+def int4_packed_bytes(outputs, inputs, group=128, zero_points=False):
+    return int(load_quantized().int4_packed_bytes(outputs, inputs, group, int(zero_points)))
+
+
+class PackedInt4Weights:
+    """Device blob of 4-bit weights [outputs, inputs], laid out for int4_linear, and what it was made for."""
+
+    def __init__(self, blob, outputs, inputs, group, scale_dtype, zero_points):
+        self.blob, self.outputs, self.inputs, self.group = blob, outputs, inputs, group
+        self.scale_dtype, self.zero_points = scale_dtype, zero_points
+
+
+def pack_int4_weights(codes, scales, zero_points=None, group=128, blob=None):
+    """codes: uint8 [outputs, inputs] with values 0..15 (the low four bits count); scales: float16 or bfloat16
+    [outputs, ceil(inputs / group)]; zero_points: uint8 of the scales' shape with values 0..15, or None for 8 throughout;
+    group: 32, 64 or 128.  A weight is scale * (code - zero_point).  Once per layer -> PackedInt4Weights."""
+    _need(codes, torch.uint8, "codes")
+    if codes.dim() != 2:
+        raise ValueError("codes have two dimensions")
+    outputs, inputs = codes.shape
+    if scales.dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError("scales must be torch.float16 or torch.bfloat16")
+    _need(scales, scales.dtype, "scales")
+    if group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64 or 128")
+    shape = (outputs, -(-inputs // group))
+    if tuple(scales.shape) != shape:
+        raise ValueError("scales must have shape %s, they have %s" % (shape, tuple(scales.shape)))
+    if zero_points is not None:
+        _need(zero_points, torch.uint8, "zero_points")
+        if tuple(zero_points.shape) != shape:
+            raise ValueError("zero_points must have the shape of scales")
+    for t in (scales, zero_points):
+        if t is not None and t.device != codes.device:
+            raise ValueError("codes, scales and zero_points must be on one device")
+    if codes.device.index != torch.cuda.current_device():
+        raise ValueError("codes are not on the current device")
+    nbytes = int4_packed_bytes(outputs, inputs, group, zero_points is not None)
+    if nbytes == 0:
+        raise WinogradError(-1 if outputs == 0 or inputs == 0 else -2, "int4_pack_weights")
+    if blob is None:
+        blob = torch.empty(nbytes, dtype=torch.uint8, device=codes.device)
+    _need(blob, torch.uint8, "blob")
+    if blob.numel() != nbytes or blob.device != codes.device:
+        raise ValueError("blob must hold %d bytes on the device of codes" % nbytes)
+    _check(load_quantized().int4_pack_weights(_ptr(codes), _ptr(scales), _TYPES[scales.dtype],
+                                              None if zero_points is None else _ptr(zero_points), outputs, inputs, group,
+                                              _ptr(blob), nbytes, _stream()), "int4_pack_weights")
+    return PackedInt4Weights(blob, outputs, inputs, group, scales.dtype, zero_points is not None)
+
+
+def int4_linear(x, packed, bias=None, relu=False, x_scale=None, out_dtype=None, out=None):
+    """relu?( x_scale * x W^T + bias ): x float16, bfloat16 or int8 [..., inputs] (two dimensions may have a row stride,
+    others are contiguous), bias float32 [outputs], x_scale float32, one per row, only with int8.  The result [..., outputs]
+    is of out_dtype: by default x's, float32 with int8.  Sums are held in 32 bits and rounded once."""
+    if type(packed) is not PackedInt4Weights:
+        raise TypeError("int4_linear needs a PackedInt4Weights, got %s" % type(packed).__name__)
+    if out_dtype is None:
+        out_dtype = torch.float32 if x.dtype == torch.int8 else x.dtype
+    return _done(_native().int4_linear_call(x, packed.blob, packed.outputs, packed.inputs, packed.group, _TYPES[packed.scale_dtype],
+                                            int(packed.zero_points), bias, int(bool(relu)), x_scale, _out_type(out_dtype, "out_dtype"), out),
+                 "int4_linear")
+
+
+# ---- a cache held in 8 bits -----------------------------------------------------------------------------------
+
+class Int8Cache:
+    """Keys and values of many sequences in blocks of `block` tokens, int8 codes with one scale per block and head:
+    k [blocks, kv_heads, block, head_dim], v [blocks, kv_heads, head_dim, block] (token by token within a head_dim: attention
+    sums over tokens), k_scale and v_scale float32 [blocks, kv_heads].  block 16, 32, 64 or 128; head_dim 64, 128 or 256."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        _need(k, torch.int8, "k")
+        if k.dim() != 4:
+            raise ValueError("k has four dimensions")
+        blocks, heads, block, dim = k.shape
+        if block not in (16, 32, 64, 128) or dim not in (64, 128, 256):
+            raise ValueError("blocks hold 16, 32, 64 or 128 tokens of 64, 128 or 256 elements, not %d of %d" % (block, dim))
+        for t, dtype, shape, what in ((v, torch.int8, (blocks, heads, dim, block), "v"), (k_scale, torch.float32, (blocks, heads), "k_scale"),
+                                      (v_scale, torch.float32, (blocks, heads), "v_scale")):
+            _need(t, dtype, what)
+            if tuple(t.shape) != shape or t.device != k.device:
+                raise ValueError("%s must have shape %s on the device of k" % (what, shape))
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+
+    blocks = property(lambda self: self.k.shape[0])
+    kv_heads = property(lambda self: self.k.shape[1])
+    block = property(lambda self: self.k.shape[2])
+    head_dim = property(lambda self: self.k.shape[3])
+
+
+def make_int8_cache(blocks, kv_heads, head_dim, block=64, device="cuda"):
+    """An empty cache (all values 0)."""
+    return Int8Cache(torch.zeros((blocks, kv_heads, block, head_dim), dtype=torch.int8, device=device),
+                     torch.zeros((blocks, kv_heads, head_dim, block), dtype=torch.int8, device=device),
+                     torch.zeros((blocks, kv_heads), dtype=torch.float32, device=device),
+                     torch.zeros((blocks, kv_heads), dtype=torch.float32, device=device))
+
+
+def _cache(cache, where):
+    if type(cache) is not Int8Cache:
+        raise TypeError("%s needs an Int8Cache, got %s" % (where, type(cache).__name__))
+    return cache.k, cache.v, cache.k_scale, cache.v_scale
+
+
+def int8_cache_append(k, v, cache, block_table, lengths, starts=None):
+    """Quantises new keys and values (float16 or bfloat16 [rows, kv_heads, head_dim], rows may lie apart) into the cache.
+
+    block_table int32 [sequences, width] names the blocks of each sequence in order, lengths int32 [sequences] its tokens, the
+    new ones included.  Rows starts[b] .. starts[b + 1] - 1 (starts int32 [sequences + 1]; None: one row per sequence) are
+    sequence b's last tokens; rows behind starts[sequences] are not looked at.  A block's scale is that of its largest value so
+    far; where it grows, the codes of the block's older tokens are brought to it.  An infinite value is stored as the type's
+    largest, NaN as 0.  Entries of block_table that name no block, and tokens beyond its width, are skipped.  Blocks that
+    receive tokens in one call have to be different ones."""
+    _check(_native().int8_cache_append_call(k, v, *_cache(cache, "int8_cache_append"), block_table, lengths, starts), "int8_cache_append")
+
+
+def int8_cache_read(cache, blocks, dtype=torch.float32):
+    """(k, v), each [len(blocks), kv_heads, block, head_dim] of `dtype`: the values that the blocks int32 [n] hold; 0 for a
+    number that names no block."""
+    return _done(_native().int8_cache_read_call(*_cache(cache, "int8_cache_read"), blocks, _out_type(dtype, "dtype")), "int8_cache_read")
+
+
+def int8_cache_attention(q, cache, block_table, lengths, starts=None, scale=None, causal=True, window=0, out=None):
+    """Softmax attention of q (float16 or bfloat16 [rows, heads, head_dim], rows may lie apart; heads a multiple of the cache's, in
+    groups) over the cache; block_table, lengths and starts as int8_cache_append takes them.  scale: of the products, by
+    default 1 / sqrt(head_dim).  causal: a row sees no token behind its own; window > 0: nor those `window` or more in front of
+    it.  A row that sees nothing gives 0; rows behind starts[sequences] are left as they were.  out must not overlap q."""
+    if scale is None:
+        scale = 1.0 / math.sqrt(cache.head_dim) if type(cache) is Int8Cache else 1.0
+    return _done(_native().int8_cache_attention_call(q, *_cache(cache, "int8_cache_attention"), block_table, lengths, starts, float(scale),
+                                                     int(bool(causal)), int(window), out), "int8_cache_attention")

@@ -93,7 +93,12 @@ int int4_linear(const void* x_dev, int x_type, long long x_stride, const float* 
     if (too_large(N, K)) return WG_EUNSUPPORTED;
     const Int4Weights w = weights_of(packed_dev, N, K, group, scale_type, has_zeros != 0);
     const Int4Output o = {x_scale_dev, bias_dev, y_dev, y_type, M, N, relu != 0};
-    return status_of(launch_int4_rows(x_dev, x_type, x_stride, w, o, static_cast<hipStream_t>(hip_stream)));
+    const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    const bool many = M > 64;
+    const auto launch = x_type == WQ_F16 ? (many ? launch_int4_tiles_half : launch_int4_rows_half)
+                      : x_type == WQ_BF16 ? (many ? launch_int4_tiles_bfloat : launch_int4_rows_bfloat)
+                                          : (many ? launch_int4_tiles_int8 : launch_int4_rows_int8);
+    return status_of(launch(x_dev, x_stride, w, o, s));
 }
 
 }  // extern "C"

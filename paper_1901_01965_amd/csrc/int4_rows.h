@@ -5,6 +5,7 @@
 // eight codes costs seven vector instructions as float16 and three as int8 (int4_weights.h), the sum over a group of sum_k x_k that
 // takes the zero points off is one more product, whose other operand is constant, and becomes the accumulator that the codes'
 // products start from.
+#pragma once
 #include "int4_weights.h"
 
 namespace wq {
@@ -13,7 +14,7 @@ namespace {
 
 constexpr int kMostWaves = 8;
 
-template <int XT, int GROUP, bool ZEROS, int MT, int NT>
+template <int XT, int GROUP, bool ZEROS, bool BF16, int MT, int NT>
 __global__ __launch_bounds__(64 * kMostWaves) void int4_rows_kernel(const typename Element<XT>::type* x, long long x_stride, Int4Weights w, Int4Output o) {
     typedef Products<XT> P;
     typedef std::conditional_t<XT == WQ_I8, v2u, v4u> Bits;
@@ -22,7 +23,7 @@ __global__ __launch_bounds__(64 * kMostWaves) void int4_rows_kernel(const typena
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int tile0 = blockIdx.x * NT, m0 = blockIdx.y * (16 * MT);
-    const bool fits = matches(w), bf16_scales = w.scale_type == WQ_BF16;
+    const bool fits = matches(w);
 
     const typename Element<XT>::type* row[MT];
 #pragma unroll
@@ -64,7 +65,7 @@ __global__ __launch_bounds__(64 * kMostWaves) void int4_rows_kernel(const typena
                 typename P::Fragment ws[kSteps];
 #pragma unroll
                 for (int j = 0; j < kSteps; ++j) ws[j] = P::weights(words[nt][g * kSteps + j]);
-                const v4f scale = load_scales<XT>(w.scales + scale_at[nt] + group, bf16_scales);
+                const v4f scale = load_scales<XT, BF16>(w.scales + scale_at[nt] + group);
                 uint32_t zeros = 0;
                 if (ZEROS) zeros = *reinterpret_cast<const uint32_t*>(w.zeros + scale_at[nt] + group);
 #pragma unroll
@@ -95,37 +96,23 @@ __global__ __launch_bounds__(64 * kMostWaves) void int4_rows_kernel(const typena
     }
 }
 
-template <int XT, int GROUP, bool ZEROS, int MT, int NT>
+template <int XT, int GROUP, bool ZEROS, bool BF16, int MT, int NT>
 hipError_t launch(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
     const dim3 grid(ceil_div(w.output_tiles, NT), ceil_div(o.M, 16 * MT));
     if (grid.y > 65535) return hipErrorInvalidValue;
     const int waves = min(kMostWaves, w.input_tiles);
-    int4_rows_kernel<XT, GROUP, ZEROS, MT, NT><<<grid, 64 * waves, 0, s>>>(static_cast<const typename Element<XT>::type*>(x), x_stride, w, o);
+    int4_rows_kernel<XT, GROUP, ZEROS, BF16, MT, NT><<<grid, 64 * waves, 0, s>>>(static_cast<const typename Element<XT>::type*>(x), x_stride, w, o);
     return hipGetLastError();
 }
 
-template <int XT, int GROUP, bool ZEROS>
-hipError_t launch_rows(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
-    if (o.M <= 16) return launch<XT, GROUP, ZEROS, 1, 1>(x, x_stride, w, o, s);
-    return launch<XT, GROUP, ZEROS, 4, 1>(x, x_stride, w, o, s);
-}
-
-template <int XT, int GROUP>
-hipError_t launch_zeros(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
-    return w.has_zeros ? launch_rows<XT, GROUP, true>(x, x_stride, w, o, s) : launch_rows<XT, GROUP, false>(x, x_stride, w, o, s);
-}
-
 template <int XT>
-hipError_t launch_group(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
-    return w.group == 32 ? launch_zeros<XT, 32>(x, x_stride, w, o, s)
-         : w.group == 64 ? launch_zeros<XT, 64>(x, x_stride, w, o, s) : launch_zeros<XT, 128>(x, x_stride, w, o, s);
+hipError_t launch_rows_of(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
+    return with_weights(w, [&](auto group, auto zeros, auto bf16) {
+        if (o.M <= 16) return launch<XT, group(), zeros(), bf16(), 1, 1>(x, x_stride, w, o, s);
+        return launch<XT, group(), zeros(), bf16(), 4, 1>(x, x_stride, w, o, s);
+    });
 }
 
 }  // namespace
-
-hipError_t launch_int4_rows(const void* x, int x_type, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
-    return x_type == WQ_F16 ? launch_group<WQ_F16>(x, x_stride, w, o, s)
-         : x_type == WQ_BF16 ? launch_group<WQ_BF16>(x, x_stride, w, o, s) : launch_group<WQ_I8>(x, x_stride, w, o, s);
-}
 
 }  // namespace wq

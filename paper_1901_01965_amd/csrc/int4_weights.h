@@ -1,5 +1,7 @@
 // How packed 4-bit weights lie in memory, and how a wave turns them into matrix-core operands.
 #pragma once
+#include <type_traits>
+
 #include "quantized_common.h"
 
 namespace wq {
@@ -148,11 +150,11 @@ __device__ inline auto load_inputs(const typename Element<XT>::type* row, int k,
 }
 
 // Scales of four neighbouring outputs, times the operands' unit.
-template <int XT>
-__device__ inline v4f load_scales(const uint16_t* p, bool bf16) {
+template <int XT, bool BF16>
+__device__ inline v4f load_scales(const uint16_t* p) {
     const v2u bits = *reinterpret_cast<const v2u*>(p);
     v4f s;
-    if (bf16) {
+    if constexpr (BF16) {
         s = v4f{__builtin_bit_cast(float, bits[0] << 16), __builtin_bit_cast(float, bits[0] & 0xffff0000u),
                 __builtin_bit_cast(float, bits[1] << 16), __builtin_bit_cast(float, bits[1] & 0xffff0000u)};
     } else {
@@ -200,6 +202,23 @@ __device__ inline void store_outputs(const Int4Output& o, int m, int n, v4f v) {
 }
 
 hipError_t launch_int4_pack(const uint8_t* codes, const void* scales, const uint8_t* zeros, const Int4Weights& w, uint8_t* blob, hipStream_t s);
-hipError_t launch_int4_rows(const void* x, int x_type, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s);
+// One translation unit per type of activations: the variants take their time to compile.
+#define WQ_DECLARE_LAUNCHERS(kind)                                                                                                       \
+    hipError_t launch_int4_##kind##_half(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s);   \
+    hipError_t launch_int4_##kind##_bfloat(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s); \
+    hipError_t launch_int4_##kind##_int8(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s);
+WQ_DECLARE_LAUNCHERS(rows)
+WQ_DECLARE_LAUNCHERS(tiles)
+#undef WQ_DECLARE_LAUNCHERS
+
+// Calls launch(group, has zero points, scales are bfloat16), each as a constant, for what the weights are.
+template <class F>
+hipError_t with_weights(const Int4Weights& w, F&& launch) {
+    auto scales = [&](auto group, auto zeros) {
+        return w.scale_type == WQ_BF16 ? launch(group, zeros, std::true_type()) : launch(group, zeros, std::false_type());
+    };
+    auto zeros = [&](auto group) { return w.has_zeros ? scales(group, std::true_type()) : scales(group, std::false_type()); };
+    return w.group == 32 ? zeros(std::integral_constant<int, 32>()) : w.group == 64 ? zeros(std::integral_constant<int, 64>()) : zeros(std::integral_constant<int, 128>());
+}
 
 }  // namespace wq

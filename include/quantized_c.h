@@ -33,13 +33,18 @@ size_t int4_packed_bytes(int N, int K, int group, int has_zeros);
 int int4_pack_weights(const uint8_t* codes_dev, const void* scales_dev, int scale_type, const uint8_t* zeros_dev, int N, int K,
                       int group, void* packed_dev, size_t packed_bytes, void* hip_stream);
 
+/* Scratch bytes int4_linear needs for such a call; 0 if it needs none or the arguments are invalid.  (Many rows are read in tiles: of
+ * rows that are not, a copy is made; bfloat16 rows become float16, times a power of two each.) */
+size_t int4_linear_workspace_bytes(const void* x_dev, int x_type, long long x_stride, int M, int K);
+
 /* x: [M][K] of x_type WQ_F16, WQ_BF16 or WQ_I8, rows x_stride elements apart (x_stride >= K).  x_scale: float [M], only for
  * WQ_I8, or NULL.  bias: float [N] or NULL.  y: dense [M][N] of y_type WQ_F16, WQ_BF16 or WQ_F32.  The blob has to be the one
  * made for these (N, K, group, scale_type, has_zeros); on a mismatch y is left untouched.  A row of x with an infinite or NaN
- * element gives NaN in that row. */
+ * element makes that row of y infinite or NaN.  workspace: int4_linear_workspace_bytes(...) bytes, scratch of this call alone while
+ * it runs. */
 int int4_linear(const void* x_dev, int x_type, long long x_stride, const float* x_scale_dev, const void* packed_dev,
                 const float* bias_dev, void* y_dev, int y_type, int M, int N, int K, int group, int scale_type, int has_zeros,
-                int relu, void* hip_stream);
+                int relu, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
 
 /* ---- a cache held in 8 bits ------------------------------------------------------------------------------------
  * A cache holds blocks of `block` (16, 32, 64 or 128) tokens of kv_heads heads of head_dim (64, 128 or 256):

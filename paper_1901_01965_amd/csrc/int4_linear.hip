@@ -50,6 +50,74 @@ __global__ void int4_pack_kernel(const uint8_t* codes, const uint16_t* scales, c
     }
 }
 
+// Rows as the kernel for many rows reads them: whole tiles of inputs with zeros behind the last, 16-byte aligned.  bfloat16 becomes
+// float16, brought by a power of two per row to a largest magnitude of 2^14 .. 2^15: its eight bits fit, down to 2^-28 of that, and
+// `factors` takes the power off again.  One workgroup per row, bound by the bytes.
+template <int XT>
+__global__ __launch_bounds__(256) void int4_rows_in_order_kernel(const typename Element<XT>::type* x, long long x_stride, typename Element<XT>::type* out,
+                                                                 float* factors, int K, int padded) {
+    typedef typename Element<XT>::type T;
+    typedef T V __attribute__((ext_vector_type(8)));
+    __shared__ float wave_largest[4];
+    const T* const row = x + (long long)blockIdx.x * x_stride;
+    T* const to = out + (long long)blockIdx.x * padded;
+    float up = 1.0f;
+    if constexpr (XT == WQ_BF16) {
+        float most = 0.0f;
+        for (int k = 8 * threadIdx.x; k < K; k += 8 * 256) {
+            const V v = __builtin_bit_cast(V, load_inputs<XT>(row, k, K, false));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf((float)v[j]));
+        }
+#pragma unroll
+        for (int step = 32; step > 0; step >>= 1) most = fmaxf(most, __shfl_xor(most, step));
+        if ((threadIdx.x & 63) == 0) wave_largest[threadIdx.x >> 6] = most;
+        __syncthreads();
+        for (int w = 0; w < 4; ++w) most = fmaxf(most, wave_largest[w]);
+        float down;
+        half_powers(most, up, down);
+        if (threadIdx.x == 0) factors[blockIdx.x] = down;
+    }
+    for (int k = 8 * threadIdx.x; k < padded; k += 8 * 256) {
+        const V v = __builtin_bit_cast(V, load_inputs<XT>(row, k, K, false));
+        if constexpr (XT == WQ_BF16) {
+            v8h h;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) h[j] = (_Float16)((float)v[j] * up);
+            *reinterpret_cast<v8h*>(to + k) = h;
+        } else {
+            *reinterpret_cast<V*>(to + k) = v;
+        }
+    }
+}
+
+hipError_t launch_rows_in_order(const void* x, int x_type, long long x_stride, void* out, float* factors, int M, int K, int padded, hipStream_t s) {
+    if (x_type == WQ_BF16)
+        int4_rows_in_order_kernel<WQ_BF16><<<M, 256, 0, s>>>(static_cast<const __bf16*>(x), x_stride, static_cast<__bf16*>(out), factors, K, padded);
+    else if (x_type == WQ_F16)
+        int4_rows_in_order_kernel<WQ_F16><<<M, 256, 0, s>>>(static_cast<const _Float16*>(x), x_stride, static_cast<_Float16*>(out), factors, K, padded);
+    else
+        int4_rows_in_order_kernel<WQ_I8><<<M, 256, 0, s>>>(static_cast<const int8_t*>(x), x_stride, static_cast<int8_t*>(out), factors, K, padded);
+    return hipGetLastError();
+}
+
+// Which kernel a call runs, and what it needs of a workspace: a copy of the rows, and one factor each.
+struct Int4Plan {
+    bool many, copy;
+    int padded;
+    size_t factors, total;   // bytes
+};
+Int4Plan plan_int4(const void* x, int x_type, long long x_stride, int M, int K) {
+    Int4Plan p = {M > 64, false, ceil_div(K, kTileInputs) * kTileInputs, 0, 0};
+    const size_t size = x_type == WQ_I8 ? 1 : 2;
+    if (!p.many) return p;
+    p.copy = x_type == WQ_BF16 || M < kTileRows || K % kTileInputs != 0 || (x_stride * size) % 16 != 0 || !aligned(x, 16) || x_stride > (1 << 24);
+    if (!p.copy) return p;
+    p.factors = (((size_t)max(M, kTileRows) * p.padded * size) + 255) & ~(size_t)255;
+    p.total = p.factors + (x_type == WQ_BF16 ? (size_t)M * sizeof(float) : 0);
+    return p;
+}
+
 }  // namespace
 
 hipError_t launch_int4_pack(const uint8_t* codes, const void* scales, const uint8_t* zeros, const Int4Weights& w, uint8_t* blob, hipStream_t s) {
@@ -79,9 +147,14 @@ int int4_pack_weights(const uint8_t* codes_dev, const void* scales_dev, int scal
     return status_of(launch_int4_pack(codes_dev, scales_dev, zeros_dev, w, static_cast<uint8_t*>(packed_dev), static_cast<hipStream_t>(hip_stream)));
 }
 
+size_t int4_linear_workspace_bytes(const void* x_dev, int x_type, long long x_stride, int M, int K) {
+    if (!(is_half(x_type) || x_type == WQ_I8) || M <= 0 || K <= 0 || K > (1 << 26)) return 0;
+    return plan_int4(x_dev, x_type, x_stride, M, K).total;
+}
+
 int int4_linear(const void* x_dev, int x_type, long long x_stride, const float* x_scale_dev, const void* packed_dev,
                 const float* bias_dev, void* y_dev, int y_type, int M, int N, int K, int group, int scale_type, int has_zeros,
-                int relu, void* hip_stream) {
+                int relu, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
     if (!packed_dev || !valid_weights(N, K, group) || !is_half(scale_type)) return WG_EINVAL;
     if (!(is_half(x_type) || x_type == WQ_I8) || !(is_half(y_type) || y_type == WQ_F32)) return WG_EINVAL;
     if (x_scale_dev && x_type != WQ_I8) return WG_EINVAL;
@@ -90,14 +163,24 @@ int int4_linear(const void* x_dev, int x_type, long long x_stride, const float* 
     if (!x_dev || !y_dev) return WG_EINVAL;
     if (!aligned(packed_dev, 256) || !aligned(y_dev, y_type == WQ_F32 ? 4 : 2) || !aligned(x_dev, x_type == WQ_I8 ? 1 : 2)) return WG_EINVAL;
     if (!aligned(x_scale_dev, 4) || !aligned(bias_dev, 4)) return WG_EINVAL;
-    if (too_large(N, K)) return WG_EUNSUPPORTED;
+    if (too_large(N, K) || M > (1 << 23)) return WG_EUNSUPPORTED;
+    const Int4Plan p = plan_int4(x_dev, x_type, x_stride, M, K);
+    if (p.total > 0) {
+        if (!workspace_dev || !aligned(workspace_dev, 256)) return WG_EINVAL;
+        if (workspace_bytes < p.total) return WG_ESMALLBUF;
+    }
     const Int4Weights w = weights_of(packed_dev, N, K, group, scale_type, has_zeros != 0);
-    const Int4Output o = {x_scale_dev, bias_dev, y_dev, y_type, M, N, relu != 0};
+    Int4Output o = {x_scale_dev, bias_dev, y_dev, y_type, M, N, relu != 0};
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    const bool many = M > 64;
-    const auto launch = x_type == WQ_F16 ? (many ? launch_int4_tiles_half : launch_int4_rows_half)
-                      : x_type == WQ_BF16 ? (many ? launch_int4_tiles_bfloat : launch_int4_rows_bfloat)
-                                          : (many ? launch_int4_tiles_int8 : launch_int4_rows_int8);
+    if (p.copy) {
+        float* const factors = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + p.factors);
+        if (hipError_t e = launch_rows_in_order(x_dev, x_type, x_stride, workspace_dev, factors, M, K, p.padded, s)) return status_of(e);
+        x_dev = workspace_dev;
+        x_stride = p.padded;
+        if (x_type == WQ_BF16) o.x_scale = factors;
+    }
+    const auto launch = p.many ? (x_type == WQ_I8 ? launch_int4_tiles_int8 : launch_int4_tiles_half)
+                      : x_type == WQ_F16 ? launch_int4_rows_half : x_type == WQ_BF16 ? launch_int4_rows_bfloat : launch_int4_rows_int8;
     return status_of(launch(x_dev, x_stride, w, o, s));
 }
 

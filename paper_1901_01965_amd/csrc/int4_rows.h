@@ -14,14 +14,14 @@ namespace {
 
 constexpr int kMostWaves = 8;
 
-template <int XT, int GROUP, bool ZEROS, bool BF16, int MT, int NT>
+template <int XT, int GROUP, bool ZEROS, bool BF16, int MT, int NT, int AHEAD>
 __global__ __launch_bounds__(64 * kMostWaves) void int4_rows_kernel(const typename Element<XT>::type* x, long long x_stride, Int4Weights w, Int4Output o) {
     typedef Products<XT> P;
     typedef std::conditional_t<XT == WQ_I8, v2u, v4u> Bits;
     constexpr int kGroups = kTileInputs / GROUP, kSteps = GROUP / 32;   // groups in a tile, products in a group
     __shared__ v4f sums[kMostWaves][NT * MT][64];
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int tile0 = blockIdx.x * NT, m0 = blockIdx.y * (16 * MT);
     const bool fits = matches(w);
 
@@ -37,22 +37,41 @@ __global__ __launch_bounds__(64 * kMostWaves) void int4_rows_kernel(const typena
         scale_at[nt] = tile * w.groups * kTileOutputs + 4 * (lane >> 4);
     }
 
-    v4f acc[NT][MT] = {};
-    const typename P::Fragment ones = P::ones(ZEROS);
-    for (int kt = wave; kt < w.input_tiles; kt += waves) {
+    // what a tile of inputs needs, on its way while earlier ones are multiplied
+    struct Stage {
         v4u words[NT];
+        v2u scales[NT][kGroups];
+        uint32_t zeros[NT][kGroups];
+        Bits x[4][MT];
+    };
+    auto load = [&](Stage& t, int kt, bool whole) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) words[nt] = codes[nt][(size_t)kt * (kTileBytes / 16)];
-        const bool whole = (kt + 1) * kTileInputs <= w.K;
-        typename P::Fragment xs[4][MT];
+        for (int nt = 0; nt < NT; ++nt) {
+            t.words[nt] = codes[nt][(size_t)kt * (kTileBytes / 16)];
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                const size_t at = scale_at[nt] + (size_t)(kt * kGroups + g) * kTileOutputs;
+                t.scales[nt][g] = *reinterpret_cast<const v2u*>(w.scales + at);
+                t.zeros[nt][g] = ZEROS ? *reinterpret_cast<const uint32_t*>(w.zeros + at) : 0;
+            }
+        }
 #pragma unroll
         for (int step = 0; step < 4; ++step)
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
-                xs[step][mt] = P::activations((Bits)load_inputs<XT>(row[mt], kt * kTileInputs + 32 * step + 8 * (lane >> 4), w.K, whole));
+                t.x[step][mt] = load_inputs<XT>(row[mt], kt * kTileInputs + 32 * step + 8 * (lane >> 4), w.K, whole);
+    };
+
+    v4f acc[NT][MT] = {};
+    const typename P::Fragment ones = P::ones(ZEROS);
+    auto multiply = [&](const Stage& t) {
+        typename P::Fragment xs[4][MT];
+#pragma unroll
+        for (int step = 0; step < 4; ++step)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) xs[step][mt] = P::activations(t.x[step][mt]);
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
-            const size_t group = (size_t)(kt * kGroups + g) * kTileOutputs;
             typename P::Sum off[MT];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
@@ -64,16 +83,14 @@ __global__ __launch_bounds__(64 * kMostWaves) void int4_rows_kernel(const typena
             for (int nt = 0; nt < NT; ++nt) {
                 typename P::Fragment ws[kSteps];
 #pragma unroll
-                for (int j = 0; j < kSteps; ++j) ws[j] = P::weights(words[nt][g * kSteps + j]);
-                const v4f scale = load_scales<XT, BF16>(w.scales + scale_at[nt] + group);
-                uint32_t zeros = 0;
-                if (ZEROS) zeros = *reinterpret_cast<const uint32_t*>(w.zeros + scale_at[nt] + group);
+                for (int j = 0; j < kSteps; ++j) ws[j] = P::weights(t.words[nt][g * kSteps + j]);
+                const v4f scale = scales_of<BF16>(t.scales[nt][g]);
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
                     typename P::Sum sum = off[mt];
                     if (ZEROS)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) sum[i] = P::times_zero(off[mt][i], (int)(zeros >> (8 * i) & 255));
+                        for (int i = 0; i < 4; ++i) sum[i] = P::times_zero(off[mt][i], (int)(t.zeros[nt][g] >> (8 * i) & 255));
 #pragma unroll
                     for (int j = 0; j < kSteps; ++j) sum = P::multiply(ws[j], xs[g * kSteps + j][mt], sum);
 #pragma unroll
@@ -81,6 +98,26 @@ __global__ __launch_bounds__(64 * kMostWaves) void int4_rows_kernel(const typena
                 }
             }
         }
+    };
+
+    const int whole_tiles = w.K / kTileInputs, count = max(whole_tiles - wave + waves - 1, 0) / waves;
+    Stage ahead[AHEAD];
+    auto tile = [&](int i) { return wave + min(i, count - 1) * waves; };
+    if (count > 0) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) load(ahead[u], tile(u), true);
+        for (int i = 0; i < count; i += AHEAD) {
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                if (i + u >= count) break;
+                multiply(ahead[u]);
+                load(ahead[u], tile(i + u + AHEAD), true);
+            }
+        }
+    }
+    if (whole_tiles < w.input_tiles && wave == whole_tiles % waves) {
+        load(ahead[0], whole_tiles, false);
+        multiply(ahead[0]);
     }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -92,7 +129,7 @@ __global__ __launch_bounds__(64 * kMostWaves) void int4_rows_kernel(const typena
         const int tile = e >> 6, l = e & 63;
         v4f total = sums[0][tile][l];
         for (int v = 1; v < waves; ++v) total += sums[v][tile][l];
-        store_outputs(o, m0 + 16 * (tile % MT) + (l & 15), (tile0 + tile / MT) * kTileOutputs + 4 * (l >> 4), total);
+        store_outputs(o, m0 + 16 * (tile % MT) + (l & 15), (tile0 + tile / MT) * kTileOutputs + 4 * (l >> 4), total, P::kUnit);
     }
 }
 
@@ -101,15 +138,18 @@ hipError_t launch(const void* x, long long x_stride, const Int4Weights& w, const
     const dim3 grid(ceil_div(w.output_tiles, NT), ceil_div(o.M, 16 * MT));
     if (grid.y > 65535) return hipErrorInvalidValue;
     const int waves = min(kMostWaves, w.input_tiles);
-    int4_rows_kernel<XT, GROUP, ZEROS, BF16, MT, NT><<<grid, 64 * waves, 0, s>>>(static_cast<const typename Element<XT>::type*>(x), x_stride, w, o);
+    constexpr int kAhead = MT * (XT == WQ_I8 ? 1 : 2) + NT <= 4 ? 4 : MT <= 2 ? 3 : 2;
+    int4_rows_kernel<XT, GROUP, ZEROS, BF16, MT, NT, kAhead><<<grid, 64 * waves, 0, s>>>(static_cast<const typename Element<XT>::type*>(x), x_stride, w, o);
     return hipGetLastError();
 }
 
 template <int XT>
 hipError_t launch_rows_of(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
     return with_weights(w, [&](auto group, auto zeros, auto bf16) {
-        if (o.M <= 16) return launch<XT, group(), zeros(), bf16(), 1, 1>(x, x_stride, w, o, s);
-        return launch<XT, group(), zeros(), bf16(), 4, 1>(x, x_stride, w, o, s);
+        const bool pairs = w.output_tiles >= 2 * kComputeUnits;
+        if (o.M <= 16) return (pairs ? launch<XT, group(), zeros(), bf16(), 1, 2> : launch<XT, group(), zeros(), bf16(), 1, 1>)(x, x_stride, w, o, s);
+        if (o.M <= 32) return (pairs ? launch<XT, group(), zeros(), bf16(), 2, 2> : launch<XT, group(), zeros(), bf16(), 2, 1>)(x, x_stride, w, o, s);
+        return (pairs ? launch<XT, group(), zeros(), bf16(), 4, 2> : launch<XT, group(), zeros(), bf16(), 4, 1>)(x, x_stride, w, o, s);
     });
 }
 

@@ -1,10 +1,15 @@
 // y = x W^T with 4-bit weights for many rows: the matrix cores' rate bounds it.
 //
-// A workgroup computes 256 outputs by 128 rows, a wave 64 of the outputs by all rows, over the inputs by tiles of 128.  Codes go from
-// memory into the wave's registers as they lie (16 bytes a lane and tile of 16 outputs) and become operands there, once per workgroup;
-// activations are shared by the waves through LDS, where the 16-byte piece c of a row r lies at c ^ (r & 15), which keeps the reads of
-// 16 rows' pieces free of bank conflicts.  The next tile's activations travel into the other half of the LDS, and its codes into
-// registers, while this one is multiplied.  A group's products are summed apart and enter the result by one multiply-add with the scale.
+// A workgroup computes 64 NT outputs by 128 rows, each of its four waves 16 NT of the outputs by all rows, over the inputs by tiles
+// of 128.  Codes go through the wave's own part of the LDS as they lie and become operands in registers, once per workgroup; activations
+// are shared by the waves through LDS, where the 16-byte piece c of a row r lies at c ^ (r & 15), which keeps the reads of 16 rows'
+// pieces free of bank conflicts.  Both travel there without registers, the next tile's while this one is multiplied.  A group's
+// products are summed apart and enter the result by one multiply-add with the scale; those of 16 rows are done between the products of
+// the next 16.  While a wave multiplies it goes ahead of the other one of its SIMD, which then unpacks codes meanwhile (270 -> 257 us
+// for 4096 rows through 4096 x 8192).
+//
+// bfloat16 activations come here as float16 (int4_linear.hip): unpacked codes then take their zero point off by a packed addition, for
+// which bfloat16 has no instruction (the product with a constant that stands in for it elsewhere took a fifth of the matrix cores).
 #pragma once
 #include "int4_weights.h"
 
@@ -13,16 +18,15 @@ namespace wq {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kWaveOutputs = 4;                               // tiles of 16
-constexpr int kOutputs = kWaves * kWaveOutputs * 16;          // of a workgroup
 constexpr int kRowTiles = 8;
-constexpr int kRows = kRowTiles * 16;
+constexpr int kRows = kTileRows;
+static_assert(kRows == 16 * kRowTiles, "rows of a tile");
+constexpr int kBand = 8;
 
 // Operands whose zero point is off already, in the order of the inputs.
-template <int XT> struct Exact { static constexpr bool kHas = false; };
+template <int XT> struct Exact;
 
 template <> struct Exact<WQ_F16> {
-    static constexpr bool kHas = true;
     __device__ static uint32_t zero(int z) {   // -(16 + z) / 16, twice
         const uint32_t h = __builtin_bit_cast(uint16_t, (_Float16)(-(16 + z) * 0.0625f));
         return h | h << 16;
@@ -35,7 +39,6 @@ template <> struct Exact<WQ_F16> {
 };
 
 template <> struct Exact<WQ_I8> {
-    static constexpr bool kHas = true;
     __device__ static uint32_t zero(int z) { return 0x04040404u * z; }
     // 4 (code - zero) in every byte: 128 + 4 code holds off a borrow, and its sign bit turned takes the 128 off again
     __device__ static long weights(uint32_t w, uint32_t zero) {
@@ -47,7 +50,7 @@ template <> struct Exact<WQ_I8> {
     }
 };
 
-template <int XT, int GROUP, bool ZEROS, bool BF16, bool WHOLE>
+template <int XT, int GROUP, bool ZEROS, bool BF16, int NT>
 __global__ __launch_bounds__(64 * kWaves, 2) void int4_tiles_kernel(const typename Element<XT>::type* x, long long x_stride, Int4Weights w, Int4Output o,
                                                                     int row_tiles, int tiles) {
     typedef typename Element<XT>::type T;
@@ -57,39 +60,35 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int4_tiles_kernel(const typena
     constexpr int kPieces = kTileInputs * sizeof(T) / 16;          // 16-byte pieces of a row of the tile
     constexpr int kLoads = kRows * kPieces / (64 * kWaves);        // a thread's
     __shared__ v4u held[2][kRows * kPieces];
-    __shared__ v4u codes[kWaves][kWaveOutputs][64];                // each wave's own
+    __shared__ v4u codes[kWaves][NT][64];                          // each wave's own
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, quarter = lane >> 4;
-    // an eighth of the tiles, one behind the other, to each of the eight XCDs, which share their codes in its L2
+    // An eighth of the tiles, one behind the other, to each of the eight XCDs, in bands of eight tiles of rows: what runs at a time there
+    // is about as high as wide, which asks least of memory behind its L2.
     const int each = tiles >> 3, rest = tiles & 7, xcd = blockIdx.x & 7;
     const int tile = xcd * each + min(xcd, rest) + (blockIdx.x >> 3);
-    const int m0 = tile % row_tiles * kRows, n_tile0 = tile / row_tiles * (kOutputs / 16) + wave * kWaveOutputs;
+    const int across = tiles / row_tiles, band = tile / (kBand * across), height = min(kBand, row_tiles - band * kBand);
+    const int in_band = tile - band * kBand * across, row_tile = band * kBand + in_band % height, column = in_band / height;
+    // the last tile of rows ends with the last row: it may share rows with the one before, which get the same values twice
+    const int m0 = max(min(row_tile * kRows, o.M - kRows), 0), n_tile0 = (column * kWaves + wave) * NT;
     const bool fits = matches(w);
     auto output_tile = [&](int nt) { return (size_t)min(n_tile0 + nt, w.output_tiles - 1); };
 
     auto fetch_codes = [&](int kt) {
 #pragma unroll
-        for (int nt = 0; nt < kWaveOutputs; ++nt)
+        for (int nt = 0; nt < NT; ++nt)
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(w.codes + (output_tile(nt) * w.input_tiles + kt) * kTileBytes + 16 * lane),
                                              (__attribute__((address_space(3))) void*)(codes[wave][nt]), 16, 0, 0);
     };
-    // thread -> (row, piece) of the tile as it lies in LDS
+    // thread -> (row, piece) of the tile as it lies in LDS: from load to load the same distance for all
+    const int my_row = threadIdx.x / kPieces, my_piece = (threadIdx.x % kPieces) ^ (my_row & (kPieces - 1));
+    const uint32_t my_bytes = (uint32_t)(my_row * x_stride * sizeof(T)) + 16 * my_piece;
     auto fetch = [&](int kt, int half) {
-        const bool whole = WHOLE || (kt + 1) * kTileInputs <= w.K;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int at = i * 64 * kWaves + threadIdx.x, r = at / kPieces, piece = (at % kPieces) ^ (r & (kPieces - 1));
-            const T* const from = x + (long long)min(m0 + r, o.M - 1) * x_stride;
-            const int k = kt * kTileInputs + piece * (16 / (int)sizeof(T));
-            if (WHOLE) {
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + k),
-                                                 (__attribute__((address_space(3))) void*)(&held[half][i * 64 * kWaves + wave * 64]), 16, 0, 0);
-            } else if constexpr (XT == WQ_I8) {
-                const v2u a = load_inputs<XT>(from, k, w.K, whole), b = load_inputs<XT>(from, k + 8, w.K, whole);
-                held[half][at] = v4u{a[0], a[1], b[0], b[1]};
-            } else {
-                held[half][at] = load_inputs<XT>(from, k, w.K, whole);
-            }
+            const char* const from = reinterpret_cast<const char*>(x + (long long)(m0 + i * 64 * kWaves / kPieces) * x_stride + kt * kTileInputs);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + my_bytes),
+                                             (__attribute__((address_space(3))) void*)(&held[half][i * 64 * kWaves + wave * 64]), 16, 0, 0);
         }
     };
     // eight inputs of row 16 mt + row, from 32 step + 8 quarter on
@@ -105,86 +104,120 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int4_tiles_kernel(const typena
         }
     };
 
-    v4f acc[kWaveOutputs][kRowTiles] = {};
+    // scales and zero points of a group, on their way while the group before is multiplied
+    struct Factors {
+        v2u scales[NT];
+        uint32_t zeros[NT];
+    };
+    auto fetch_factors = [&](Factors& f, int group) {
+        const size_t first = (size_t)min(group, w.input_tiles * kGroups - 1) * kTileOutputs;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const size_t at = output_tile(nt) * w.groups * kTileOutputs + first;
+            f.scales[nt] = *reinterpret_cast<const v2u*>(w.scales + at + 4 * quarter);
+            f.zeros[nt] = 0;
+            if (ZEROS) f.zeros[nt] = w.zeros[at + row];
+        }
+    };
+
+    v4f acc[NT][kRowTiles] = {};
+    Factors next;
     fetch_codes(0);
     fetch(0, 0);
+    fetch_factors(next, 0);
     for (int kt = 0; kt < w.input_tiles; ++kt) {
         const int half = kt & 1;
-        __syncthreads();   // this tile is there, the other half has been read
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's share of the tile is there
+        __syncthreads();                                   // everyone's is, and the other half has been read
         if (kt + 1 < w.input_tiles) fetch(kt + 1, half ^ 1);
 #pragma unroll 1
-        for (int g = 0; g < kGroups; ++g) {
-            const size_t group = (size_t)(kt * kGroups + g) * kTileOutputs;
-            typename P::Fragment ws[kWaveOutputs][kSteps];
-            v4f scale[kWaveOutputs];
-            uint32_t zeros[kWaveOutputs];
+        for (int group = 0; group < kGroups; ++group) {
+            typename P::Fragment ws[NT][kSteps];
+            const Factors now = next;
 #pragma unroll
-            for (int nt = 0; nt < kWaveOutputs; ++nt) {
-                const size_t scale_at = output_tile(nt) * w.groups * kTileOutputs + group;
-                scale[nt] = load_scales<XT, BF16>(w.scales + scale_at + 4 * quarter);
-                uint32_t zero = 0;
-                if constexpr (E::kHas) zero = E::zero(ZEROS ? w.zeros[scale_at + row] : 8);
-                else if (ZEROS) zeros[nt] = *reinterpret_cast<const uint32_t*>(w.zeros + scale_at + 4 * quarter);
-                const uint32_t* const words = reinterpret_cast<const uint32_t*>(&codes[wave][nt][lane]) + g * kSteps;
+            for (int nt = 0; nt < NT; ++nt) {
+                const uint32_t zero = E::zero(ZEROS ? (int)now.zeros[nt] : 8);
+                const uint32_t* const words = reinterpret_cast<const uint32_t*>(&codes[wave][nt][lane]) + group * kSteps;
 #pragma unroll
-                for (int j = 0; j < kSteps; ++j) {
-                    if constexpr (E::kHas) ws[nt][j] = E::weights(words[j], zero);
-                    else ws[nt][j] = P::weights(words[j]);
-                }
+                for (int j = 0; j < kSteps; ++j) ws[nt][j] = E::weights(words[j], zero);
             }
-            if (g == kGroups - 1 && kt + 1 < w.input_tiles) fetch_codes(kt + 1);
+            __builtin_amdgcn_sched_barrier(0);   // the codes are read before the next ones are asked for in their place
+            if (group == kGroups - 1 && kt + 1 < w.input_tiles) fetch_codes(kt + 1);
+            v4f scale[NT];
 #pragma unroll
-            for (int mt = 0; mt < kRowTiles; ++mt) {
-                typename P::Fragment xs[kSteps];
+            for (int nt = 0; nt < NT; ++nt) scale[nt] = scales_of<BF16>(now.scales[nt]);
+            fetch_factors(next, kt * kGroups + group + 1);
+            typename P::Fragment xs[2][kSteps];
 #pragma unroll
-                for (int j = 0; j < kSteps; ++j) xs[j] = inputs(half, mt, g * kSteps + j);
-                typename P::Sum off = {};
-                if constexpr (!E::kHas) {
-                    const typename P::Fragment ones = P::ones(ZEROS);
+            for (int j = 0; j < kSteps; ++j) xs[0][j] = inputs(half, 0, group * kSteps + j);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+            // the products of 16 rows, and between them the multiply-adds of the 16 before
+            typename P::Sum sums[2][NT];
 #pragma unroll
-                    for (int j = 0; j < kSteps; ++j) off = P::multiply(ones, xs[j], off);
+            for (int mt = 0; mt <= kRowTiles; ++mt) {
+                if (mt + 1 < kRowTiles)
+#pragma unroll
+                    for (int j = 0; j < kSteps; ++j) xs[(mt + 1) & 1][j] = inputs(half, mt + 1, group * kSteps + j);
+                if (mt < kRowTiles) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) sums[mt & 1][nt] = typename P::Sum{};
+#pragma unroll
+                    for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) sums[mt & 1][nt] = P::multiply(ws[nt][j], xs[mt & 1][j], sums[mt & 1][nt]);
                 }
+                if (mt > 0)
 #pragma unroll
-                for (int nt = 0; nt < kWaveOutputs; ++nt) {
-                    typename P::Sum sum = off;
-                    if constexpr (!E::kHas && ZEROS)
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) sum[i] = P::times_zero(off[i], (int)(zeros[nt] >> (8 * i) & 255));
+                        for (int i = 0; i < 4; ++i)
+                            acc[nt][mt - 1][i] = __builtin_fmaf((float)sums[(mt - 1) & 1][nt][i], scale[nt][i], acc[nt][mt - 1][i]);
+                if (mt > 0 && mt < kRowTiles)
 #pragma unroll
-                    for (int j = 0; j < kSteps; ++j) sum = P::multiply(ws[nt][j], xs[j], sum);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[nt][mt][i] = __builtin_fmaf((float)sum[i], scale[nt][i], acc[nt][mt][i]);
-                }
+                    for (int i = 0; i < kSteps * NT; ++i) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // a product
+                        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // a read of LDS
+                        __builtin_amdgcn_sched_group_barrier(0x002, 4 / kSteps, 0);
+                    }
                 __builtin_amdgcn_sched_barrier(0);
             }
+            __builtin_amdgcn_s_setprio(0);
         }
     }
     if (!fits) return;
 #pragma unroll
     for (int mt = 0; mt < kRowTiles; ++mt)
 #pragma unroll
-        for (int nt = 0; nt < kWaveOutputs; ++nt)
-            store_outputs(o, m0 + 16 * mt + row, (n_tile0 + nt) * kTileOutputs + 4 * quarter, acc[nt][mt]);
+        for (int nt = 0; nt < NT; ++nt)
+            store_outputs(o, m0 + 16 * mt + row, (n_tile0 + nt) * kTileOutputs + 4 * quarter, acc[nt][mt], P::kUnit);
 }
 
-template <int XT, int GROUP, bool ZEROS, bool BF16>
+template <int XT, int GROUP, bool ZEROS, bool BF16, int NT>
 hipError_t launch(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
-    typedef typename Element<XT>::type T;
     const int row_tiles = ceil_div(o.M, kRows);
-    const long long tiles = (long long)row_tiles * ceil_div(w.N, kOutputs);
+    const long long tiles = (long long)row_tiles * ceil_div(w.output_tiles, kWaves * NT);
     if (tiles > (1 << 23)) return hipErrorInvalidValue;
-    // loads straight into LDS move whole, aligned pieces
-    const bool whole = w.K % kTileInputs == 0 && (x_stride * sizeof(T)) % 16 == 0 && aligned(x, 16);
-    if (whole)
-        int4_tiles_kernel<XT, GROUP, ZEROS, BF16, true><<<(unsigned)tiles, 64 * kWaves, 0, s>>>(static_cast<const T*>(x), x_stride, w, o, row_tiles, (int)tiles);
-    else
-        int4_tiles_kernel<XT, GROUP, ZEROS, BF16, false><<<(unsigned)tiles, 64 * kWaves, 0, s>>>(static_cast<const T*>(x), x_stride, w, o, row_tiles, (int)tiles);
+    int4_tiles_kernel<XT, GROUP, ZEROS, BF16, NT><<<(unsigned)tiles, 64 * kWaves, 0, s>>>(static_cast<const typename Element<XT>::type*>(x), x_stride, w, o,
+                                                                                        row_tiles, (int)tiles);
     return hipGetLastError();
+}
+
+// Rounds of two workgroups per compute unit that this many outputs a wave take.
+inline long long rounds(const Int4Weights& w, const Int4Output& o, int nt) {
+    return ((long long)ceil_div(o.M, kRows) * ceil_div(w.output_tiles, kWaves * nt) + 2 * kComputeUnits - 1) / (2 * kComputeUnits);
 }
 
 template <int XT>
 hipError_t launch_tiles_of(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
-    return with_weights(w, [&](auto group, auto zeros, auto bf16) { return launch<XT, group(), zeros(), bf16()>(x, x_stride, w, o, s); });
+    return with_weights(w, [&](auto group, auto zeros, auto bf16) {
+        // Three tiles of outputs a wave ask a third less of the LDS per product than two, which bounds float16 (8192 rows through
+        // 4096 x 28672: 1710 against 1850 us; int8 asks half as much: 210 against 190 us for 4096 rows through 4096 x 8192), where their
+        // coarser rounds do not cost more (2048 rows through 4096 x 4096: 80 against 67 us).
+        if constexpr (XT == WQ_F16)
+            if (rounds(w, o, 3) * 1.5 * 0.92 < rounds(w, o, 2)) return launch<XT, group(), zeros(), bf16(), 3>(x, x_stride, w, o, s);
+        return launch<XT, group(), zeros(), bf16(), 2>(x, x_stride, w, o, s);
+    });
 }
 
 }  // namespace

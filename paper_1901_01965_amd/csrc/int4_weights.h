@@ -16,6 +16,7 @@ namespace wq {
 // bits of its fraction: masked there and joined with the bits of 1.0 it reads as 1 + code / 16, exactly, without a conversion.
 constexpr int kTileOutputs = 16;
 constexpr int kTileInputs = 128;
+constexpr int kTileRows = 128;   // of the kernel for many rows
 constexpr int kTileBytes = kTileOutputs * kTileInputs / 2;
 
 constexpr uint32_t kInt4Magic = 0x34695157u;
@@ -58,6 +59,13 @@ __device__ inline bool matches(const Int4Weights& w) {
            (h->scale_type == w.scale_type) & (h->has_zeros == w.has_zeros);
 }
 
+// (w & mask) | bits in one instruction, for which a constant each has to lie in a scalar and a vector register.
+__device__ inline uint32_t masked(uint32_t w, uint32_t mask, uint32_t bits) {
+    uint32_t r;
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(w), "s"(mask), "v"(bits));
+    return r;
+}
+
 __device__ inline uint32_t rotate_right(uint32_t w, int bits) { return __builtin_amdgcn_alignbit(w, w, bits); }
 
 // What the products of one type of activations are made of.  A code u enters as a x16 or x4 multiple of itself plus a constant:
@@ -72,7 +80,7 @@ template <> struct Products<WQ_F16> {
     static constexpr int kOffset = 16;
     __device__ static Fragment weights(uint32_t w) {
         const uint32_t field = 0x03c003c0u, one = 0x3c003c00u;
-        const v4u r = {((w << 4) & field) | one, (w & field) | one, ((w >> 4) & field) | one, (rotate_right(w, 8) & field) | one};
+        const v4u r = {masked(w << 4, field, one), masked(w, field, one), masked(w >> 4, field, one), masked(rotate_right(w, 8), field, one)};
         return __builtin_bit_cast(Fragment, r);
     }
     // the same value in every place: -(16 + 8) / 16 where the zero point is 8 everywhere, else -1 / 16
@@ -95,7 +103,7 @@ template <> struct Products<WQ_BF16> {
     static constexpr int kOffset = 16;
     __device__ static Fragment weights(uint32_t w) {
         const uint32_t field = 0x00780078u, one = 0x3f803f80u;
-        const v4u r = {((w << 1) & field) | one, ((w >> 3) & field) | one, ((w >> 7) & field) | one, (rotate_right(w, 11) & field) | one};
+        const v4u r = {masked(w << 1, field, one), masked(w >> 3, field, one), masked(w >> 7, field, one), masked(rotate_right(w, 11), field, one)};
         return __builtin_bit_cast(Fragment, r);
     }
     __device__ static Fragment ones(bool zeros) {
@@ -149,10 +157,9 @@ __device__ inline auto load_inputs(const typename Element<XT>::type* row, int k,
     return r.bits;
 }
 
-// Scales of four neighbouring outputs, times the operands' unit.
-template <int XT, bool BF16>
-__device__ inline v4f load_scales(const uint16_t* p) {
-    const v2u bits = *reinterpret_cast<const v2u*>(p);
+// The scales of four neighbouring outputs.
+template <bool BF16>
+__device__ inline v4f scales_of(v2u bits) {
     v4f s;
     if constexpr (BF16) {
         s = v4f{__builtin_bit_cast(float, bits[0] << 16), __builtin_bit_cast(float, bits[0] & 0xffff0000u),
@@ -161,7 +168,7 @@ __device__ inline v4f load_scales(const uint16_t* p) {
         const v4h h = __builtin_bit_cast(v4h, bits);
         s = v4f{(float)h[0], (float)h[1], (float)h[2], (float)h[3]};
     }
-    return s * Products<XT>::kUnit;
+    return s;
 }
 
 // What becomes of a finished sum: the row's scale, bias, ReLU, one rounding.
@@ -172,8 +179,10 @@ struct Int4Output {
     int type, M, N, relu;
 };
 
-__device__ inline void store_outputs(const Int4Output& o, int m, int n, v4f v) {
+// unit: the operands'.
+__device__ inline void store_outputs(const Int4Output& o, int m, int n, v4f v, float unit) {
     if (m >= o.M || n >= o.N) return;
+    v *= unit;
     if (o.x_scale) v *= o.x_scale[m];
     const long long at = (long long)m * o.N + n;
     float r[4];
@@ -203,13 +212,12 @@ __device__ inline void store_outputs(const Int4Output& o, int m, int n, v4f v) {
 
 hipError_t launch_int4_pack(const uint8_t* codes, const void* scales, const uint8_t* zeros, const Int4Weights& w, uint8_t* blob, hipStream_t s);
 // One translation unit per type of activations: the variants take their time to compile.
-#define WQ_DECLARE_LAUNCHERS(kind)                                                                                                       \
-    hipError_t launch_int4_##kind##_half(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s);   \
-    hipError_t launch_int4_##kind##_bfloat(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s); \
-    hipError_t launch_int4_##kind##_int8(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s);
-WQ_DECLARE_LAUNCHERS(rows)
-WQ_DECLARE_LAUNCHERS(tiles)
-#undef WQ_DECLARE_LAUNCHERS
+hipError_t launch_int4_rows_half(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s);
+hipError_t launch_int4_rows_bfloat(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s);
+hipError_t launch_int4_rows_int8(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s);
+// Many rows: x holds whole tiles (kTileInputs inputs, kTileRows rows or more) of 16-byte aligned rows.
+hipError_t launch_int4_tiles_half(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s);
+hipError_t launch_int4_tiles_int8(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s);
 
 // Calls launch(group, has zero points, scales are bfloat16), each as a constant, for what the weights are.
 template <class F>

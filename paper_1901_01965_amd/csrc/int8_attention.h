@@ -33,19 +33,6 @@ __device__ inline v8h codes_to_half(uint32_t a, uint32_t b) {
     return v8h{r[0][0], r[0][1], r[1][0], r[1][1], r[2][0], r[2][1], r[3][0], r[3][1]};
 }
 
-// What a query's element is multiplied with so that it can be held as float16: a power of two that brings the row's largest magnitude
-// to 2^14 .. 2^15 (a bfloat16's eight bits then fit, down to 2^-29 of the largest), and its inverse.  Float16 is held as it is.
-template <int TYPE>
-__device__ inline void query_powers(float largest, float& up, float& down) {
-    if (TYPE == WQ_F16) {
-        up = down = 1.0f;
-        return;
-    }
-    const int e = max((int)(__builtin_bit_cast(uint32_t, largest) >> 23), 15);   // 127 + exponent; 255: infinite, stays it
-    up = __builtin_bit_cast(float, (uint32_t)(268 - e) << 23);
-    down = __builtin_bit_cast(float, (uint32_t)(e - 14) << 23);
-}
-
 // The tokens that a row at `position` sees: low .. high - 1.
 __device__ inline void visible(const AttentionArgs& a, int position, int length, int& low, int& high) {
     high = position < 0 ? 0 : a.causal ? min(position + 1, length) : length;

@@ -96,8 +96,8 @@ __global__ __launch_bounds__(64 * kWaves) void int8_attention_kernel(AttentionAr
     }
     most = fmaxf(most, __shfl_xor(most, 16));
     most = fmaxf(most, __shfl_xor(most, 32));
-    float up, down;
-    query_powers<TYPE>(most, up, down);
+    float up = 1.0f, down = 1.0f;
+    if (TYPE == WQ_BF16) half_powers(most, up, down);
     v8h qs[D / 32];
 #pragma unroll
     for (int f = 0; f < D / 32; ++f)

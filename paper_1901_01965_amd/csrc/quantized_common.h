@@ -36,6 +36,14 @@ template <> struct Element<WQ_BF16> { typedef __bf16 type; };
 template <> struct Element<WQ_I8> { typedef int8_t type; };
 template <> struct Element<WQ_F32> { typedef float type; };
 
+// What a row of bfloat16 elements is multiplied with so that float16 holds them: a power of two that brings the largest magnitude to
+// 2^14 .. 2^15 (its eight bits then fit, down to 2^-28 of the largest), and the inverse.  An infinite magnitude stays it.
+__device__ inline void half_powers(float largest, float& up, float& down) {
+    const int e = max((int)(__builtin_bit_cast(uint32_t, largest) >> 23), 15);   // 127 + exponent
+    up = __builtin_bit_cast(float, (uint32_t)(268 - e) << 23);
+    down = __builtin_bit_cast(float, (uint32_t)(e - 14) << 23);
+}
+
 inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 inline int status_of(hipError_t e) { return e == hipSuccess ? WG_OK : WG_ERUNTIME; }
 inline bool is_half(int type) { return type == WQ_F16 || type == WQ_BF16; }

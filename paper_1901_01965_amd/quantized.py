@@ -16,7 +16,7 @@ from .binding import WinogradError, _check, _done, _native, _need, _ptr, _stream
 F16, BF16, I8, F32 = 0, 1, 2, 3
 _TYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
 
-EXPORTED_SYMBOLS = ("int4_packed_bytes", "int4_pack_weights", "int4_linear", "int8_cache_append", "int8_cache_read",
+EXPORTED_SYMBOLS = ("int4_packed_bytes", "int4_pack_weights", "int4_linear_workspace_bytes", "int4_linear", "int8_cache_append", "int8_cache_read",
                     "int8_cache_attention_workspace_bytes", "int8_cache_attention")
 
 _ready = None
@@ -32,7 +32,8 @@ def load_quantized():
         sigs = {
             "int4_packed_bytes": (sz, [i] * 4),
             "int4_pack_weights": (i, [vp, vp, i, vp, i, i, i, vp, sz, vp]),
-            "int4_linear": (i, [vp, i, ll, vp, vp, vp, vp] + [i] * 8 + [vp]),
+            "int4_linear_workspace_bytes": (sz, [vp, i, ll, i, i]),
+            "int4_linear": (i, [vp, i, ll, vp, vp, vp, vp] + [i] * 8 + [vp, sz, vp]),
             "int8_cache_append": (i, [vp, ll, vp, ll, i, i] + cache + batch + [vp]),
             "int8_cache_read": (i, cache + [vp, i, vp, vp, i, vp]),
             "int8_cache_attention_workspace_bytes": (sz, [i] * 8),

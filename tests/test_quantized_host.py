@@ -56,8 +56,9 @@ def test_weights_are_refused_before_any_launch(lib):
 
 
 def test_products_are_refused_before_any_launch(lib):
-    def call(x=A, x_type=F16, stride=128, x_scale=None, blob=B, bias=None, y=C, y_type=F16, M=4, N=16, K=128, group=64, scale_type=F16, relu=0):
-        return lib.int4_linear(x, x_type, stride, x_scale, blob, bias, y, y_type, M, N, K, group, scale_type, 0, relu, None)
+    def call(x=A, x_type=F16, stride=128, x_scale=None, blob=B, bias=None, y=C, y_type=F16, M=4, N=16, K=128, group=64, scale_type=F16, relu=0,
+             workspace=None, size=0):
+        return lib.int4_linear(x, x_type, stride, x_scale, blob, bias, y, y_type, M, N, K, group, scale_type, 0, relu, workspace, size, None)
     assert call(x=None) == call(blob=None) == call(y=None) == EINVAL
     assert call(x_type=F32) == call(x_type=7) == call(y_type=I8) == call(scale_type=I8) == EINVAL
     assert call(stride=127) == call(M=-1) == call(N=0) == call(group=100) == EINVAL
@@ -65,6 +66,14 @@ def test_products_are_refused_before_any_launch(lib):
     assert call(x=ODD) == call(y=ODD) == call(y=p(0x30002), y_type=F32) == call(blob=p(0x20080)) == call(bias=p(0x20002)) == EINVAL
     assert call(K=1 << 27, stride=1 << 27) == EUNSUPPORTED
     assert call(M=0, x=None, y=None) == OK
+    assert call(M=1 << 24) == EUNSUPPORTED
+    need = lambda **a: lib.int4_linear_workspace_bytes(*dict(dict(x=A, x_type=BF16, stride=128, M=300, K=128), **a).values())
+    assert need() == 300 * 128 * 2 + 300 * 4
+    assert call(M=300, x_type=BF16) == call(M=300, x_type=BF16, workspace=p(0x40010), size=1 << 40) == EINVAL
+    assert call(M=300, x_type=BF16, workspace=D, size=need() - 1) == ESMALLBUF
+    assert need(M=4) == need(x_type=F16) == need(x_type=F32) == need(M=0) == 0   # few rows; whole, aligned tiles; invalid
+    for copied in (dict(K=120), dict(stride=129), dict(x=p(0x10002)), dict(M=100)):
+        assert need(x_type=F16, **copied) > 0
 
 
 def cache_args(**over):

@@ -13,9 +13,10 @@ struct AttentionArgs {
     const float *k_scale, *v_scale;
     float* partial;   // sums of parts of the tokens, where a sequence is split
     Batch batch;
-    int kv_heads, group;   // heads of queries per head of keys
+    int kv_heads, group;               // heads of queries per head of keys
+    int tile_rows, unit, head_tiles;   // a workgroup's rows: up to `unit` of a sequence's, of a group's heads or tile_rows of them
     int causal, window, splits;
-    float scale_log2;      // scale / ln 2: exponentials are taken to base 2
+    float scale_log2, sign;            // |scale| / ln 2: exponentials are taken to base 2
 };
 
 // Four codes as two pairs of float16, exactly: a byte with its sign bit turned is code + 128, and in the fraction of 1024 it counts
@@ -51,15 +52,50 @@ __device__ inline void store4(void* out, long long at, v4f v) {
     store_unaligned<2>(static_cast<T*>(out) + at, V{(T)v[0], (T)v[1], (T)v[2], (T)v[3]});
 }
 
+constexpr int kStep = 64;        // tokens a wave or workgroup takes at a time
+constexpr int kLeastSteps = 4;   // of a part of a sequence
+
+// A tile's rows and tokens.
+struct Tile {
+    Sequence sequence;
+    int s, token0, tokens;      // its first row in the sequence, rows
+    int head0, heads;           // first head of queries, heads
+    int begin, steps, per;      // tokens from `begin` on in steps of kStep, of which a part has `per`
+    int low, high;              // tokens that any row sees
+    int low_all, high_all;      // tokens that every row sees, unless low_all >= high_all
+};
+
+__device__ inline bool tile_of(const AttentionArgs& a, int item, int y, Tile& t) {
+    const Batch& b = a.batch;
+    t.s = b.starts ? sequence_of_item(b, item, a.unit, 1) : item;
+    t.sequence = sequence_of(b, t.s);
+    t.token0 = b.starts ? (item - item_base(b, t.s, a.unit, 1)) * a.unit : 0;
+    if (t.token0 < 0 || t.token0 >= t.sequence.count) return false;
+    t.tokens = min(a.unit, t.sequence.count - t.token0);
+    const int tile = y % a.head_tiles;
+    t.head0 = y / a.head_tiles * a.group + a.tile_rows * tile;
+    t.heads = min(a.group - a.tile_rows * tile, a.tile_rows);
+    const int position = t.sequence.length - t.sequence.count + t.token0;
+    visible(a, position, t.sequence.length, t.low, t.high_all);
+    visible(a, position + t.tokens - 1, t.sequence.length, t.low_all, t.high);
+    t.begin = t.low & ~(kStep - 1);
+    t.steps = max(ceil_div(t.high - t.begin, kStep), 0);
+    t.per = ceil_div(t.steps, min(a.splits, max(t.steps / kLeastSteps, 1)));
+    return true;
+}
+
 struct AttentionPlan {
-    int tokens_shift;   // a tile of 16 rows holds 1 << tokens_shift of a sequence's rows, of up to 16 heads each
-    int head_tiles;     // tiles of 16 that a group of heads needs
-    long long items;    // tiles of rows, head tiles aside
+    bool many;
+    int tile_rows, unit, head_tiles;
+    long long items;   // tiles of rows, those of a group's heads aside
     int splits;
     size_t workspace;
 };
-AttentionPlan plan_attention(int rows, int heads, int kv_heads, int head_dim, int block, int width, int sequences, bool has_starts);
+
+// Rows of a workgroup of the kernel for many rows.
+constexpr int many_rows(int head_dim) { return head_dim == 256 ? 64 : 192; }
 
 hipError_t launch_attention_rows(const AttentionArgs& a, const AttentionPlan& p, int type, int head_dim, hipStream_t s);
+hipError_t launch_attention_many(const AttentionArgs& a, const AttentionPlan& p, int type, int head_dim, hipStream_t s);
 
 }  // namespace wq

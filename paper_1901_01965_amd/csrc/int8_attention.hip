@@ -1,0 +1,124 @@
+// Attention over the cache held in 8 bits: C ABI, choice of the kernel, and the joining of a sequence's parts.
+#include <cmath>
+
+#include "int8_attention.h"
+
+namespace wq {
+
+namespace {
+
+// Joins the parts of a row: one workgroup per row, its threads share the parts out.
+template <int TYPE, int D>
+__global__ __launch_bounds__(256) void int8_attention_join_kernel(AttentionArgs a) {
+    constexpr int kAcross = D / 4, kDown = 256 / kAcross;
+    __shared__ v4f sums[kDown][kAcross];
+    __shared__ float totals[kDown];
+    Tile t;
+    if (!tile_of(a, blockIdx.x / a.tile_rows, blockIdx.y, t)) return;
+    const int row = blockIdx.x % a.tile_rows;
+    if (row >= t.tokens * t.heads || t.per >= t.steps) return;
+    const int parts = ceil_div(t.steps, t.per), across = threadIdx.x % kAcross, down = threadIdx.x / kAcross;
+    const long long each = a.tile_rows * (D + 2);
+    const float* const partial = a.partial + ((long long)(blockIdx.x / a.tile_rows) * gridDim.y + blockIdx.y) * a.splits * each;
+    float all = -INFINITY;
+    for (int p = 0; p < parts; ++p) all = fmaxf(all, partial[p * each + a.tile_rows * D + 2 * row]);
+    v4f r = {};
+    float total = 0.0f;
+    for (int p = down; p < parts; p += kDown) {
+        const float* const part = partial + p * each;
+        const float largest = part[a.tile_rows * D + 2 * row];
+        const float factor = largest == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(largest - all);
+        if (largest != -INFINITY) total += part[a.tile_rows * D + 2 * row + 1] * factor;
+        r += *reinterpret_cast<const v4f*>(part + row * D + 4 * across) * factor;
+    }
+    sums[down][across] = r;
+    if (across == 0) totals[down] = total;
+    __syncthreads();
+    if (down != 0) return;
+    for (int i = 1; i < kDown; ++i) {
+        r += sums[i][across];
+        total += totals[i];
+    }
+    const float over = total == 0.0f ? 0.0f : 1.0f / total;
+    const long long row_at = (long long)(t.sequence.first + t.token0 + row / t.heads);
+    store4<TYPE>(a.out, row_at * a.out_stride + (long long)(t.head0 + row % t.heads) * D + 4 * across, r * over);
+}
+
+template <int TYPE, int D>
+hipError_t join(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) {
+    int8_attention_join_kernel<TYPE, D><<<dim3((unsigned)(p.items * p.tile_rows), a.kv_heads * a.head_tiles), 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_join(const AttentionArgs& a, const AttentionPlan& p, int type, int head_dim, hipStream_t s) {
+    if (type == WQ_F16) return head_dim == 64 ? join<WQ_F16, 64>(a, p, s) : head_dim == 128 ? join<WQ_F16, 128>(a, p, s) : join<WQ_F16, 256>(a, p, s);
+    return head_dim == 64 ? join<WQ_BF16, 64>(a, p, s) : head_dim == 128 ? join<WQ_BF16, 128>(a, p, s) : join<WQ_BF16, 256>(a, p, s);
+}
+
+AttentionPlan plan_attention(int rows, int heads, int kv_heads, int head_dim, int block, int width, int sequences, bool has_starts) {
+    AttentionPlan p;
+    const int group = heads / kv_heads;
+    // few rows of a sequence for the kernel that reads the cache once for 16 rows; more for the one that shares it among many
+    p.many = has_starts && group <= 64 && (long long)rows * group >= 64ll * sequences;
+    p.tile_rows = p.many ? many_rows(head_dim) : 16;
+    p.head_tiles = p.many ? 1 : ceil_div(group, 16);
+    p.unit = 1;
+    if (p.many) p.unit = p.tile_rows / group;
+    else
+        while (has_starts && 2 * p.unit * group <= 16) p.unit *= 2;
+    p.items = has_starts ? item_count(rows, sequences, p.unit, 1) : sequences;
+    const long long tiles = p.items * kv_heads * p.head_tiles;
+    const long long most = max((long long)width * block / (kStep * kLeastSteps), 1ll);
+    p.splits = (int)min(max(((p.many ? 2ll : 8ll) * kComputeUnits + tiles - 1) / tiles, 1ll), most);
+    p.workspace = p.splits > 1 ? (size_t)tiles * p.splits * p.tile_rows * (head_dim + 2) * sizeof(float) : 0;
+    return p;
+}
+
+}  // namespace
+
+}  // namespace wq
+
+using namespace wq;
+
+extern "C" {
+
+size_t int8_cache_attention_workspace_bytes(int rows, int heads, int kv_heads, int head_dim, int block, int table_width,
+                                            int sequences, int has_starts) {
+    if (rows <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || table_width <= 0 || sequences <= 0) return 0;
+    if ((head_dim != 64 && head_dim != 128 && head_dim != 256) || (block != 16 && block != 32 && block != 64 && block != 128)) return 0;
+    return plan_attention(rows, heads, kv_heads, head_dim, block, table_width, sequences, has_starts != 0).workspace;
+}
+
+int int8_cache_attention(const void* q_dev, long long q_stride, int type, int rows, int heads, const int8_t* cache_k_dev,
+                         const int8_t* cache_v_dev, const float* k_scale_dev, const float* v_scale_dev, int blocks, int kv_heads,
+                         int head_dim, int block, const int32_t* table_dev, int table_width, int sequences,
+                         const int32_t* lengths_dev, const int32_t* starts_dev, float scale, int causal, int window, void* out_dev,
+                         long long out_stride, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+    const CacheArgs c = {cache_k_dev, cache_v_dev, k_scale_dev, v_scale_dev, blocks, kv_heads, head_dim, block};
+    if (int st = check_cache(c)) return st;
+    bool empty;
+    if (int st = check_batch(rows, table_dev, table_width, sequences, lengths_dev, starts_dev, block, empty)) return st;
+    if (!is_half(type) || heads <= 0 || heads % kv_heads || window < 0 || (window > 0 && !causal)) return WG_EINVAL;
+    if (!(scale - scale == 0.0f)) return WG_EINVAL;   // infinite or NaN
+    if (heads > 8192) return WG_EUNSUPPORTED;
+    if (q_stride < (long long)heads * head_dim || out_stride < (long long)heads * head_dim) return WG_EINVAL;
+    if (empty) return WG_OK;
+    if (!q_dev || !out_dev || !aligned(q_dev, 2) || !aligned(out_dev, 2)) return WG_EINVAL;
+    const AttentionPlan p = plan_attention(rows, heads, kv_heads, head_dim, block, table_width, sequences, starts_dev != nullptr);
+    if (p.items * max(p.splits, p.splits > 1 ? p.tile_rows : 1) > kMostItems) return WG_EUNSUPPORTED;
+    if (p.workspace > 0) {
+        if (!workspace_dev || !aligned(workspace_dev, 256)) return WG_EINVAL;
+        if (workspace_bytes < p.workspace) return WG_ESMALLBUF;
+    }
+    // a negative scale goes into the queries' sign
+    const AttentionArgs a = {q_dev, q_stride, out_dev, out_stride, cache_k_dev, cache_v_dev, k_scale_dev, v_scale_dev,
+                             static_cast<float*>(workspace_dev),
+                             {table_dev, lengths_dev, starts_dev, table_width, sequences, rows, blocks, block_shift(block)},
+                             kv_heads, heads / kv_heads, p.tile_rows, p.unit, p.head_tiles, causal != 0, window, p.splits,
+                             fabsf(scale) * 1.44269504088896340736f, scale < 0.0f ? -1.0f : 1.0f};
+    const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    if (hipError_t e = (p.many ? launch_attention_many : launch_attention_rows)(a, p, type, head_dim, s)) return status_of(e);
+    return status_of(p.splits > 1 ? launch_join(a, p, type, head_dim, s) : hipSuccess);
+}
+
+}  // extern "C"

@@ -1,0 +1,326 @@
+// Attention over the cache held in 8 bits, for many rows per sequence: prompts.
+//
+// A workgroup takes 64 RT rows that read the same head of keys (the heads of a group, times tokens), each of its four waves 16 RT of
+// them.  Tiles of TOKENS tokens are turned into float16 once per workgroup on their way into LDS (exactly, as in the kernel for few
+// rows, whose arithmetic and orders of tokens this one shares) while the tile before is worked on.  The vector instructions of the
+// softmax bound it next to the matrix cores, so an element costs six of them and its exponential: the largest score is sought before
+// the scale is multiplied in, the scale of the key and the lowering are one multiply-add, the value's scale is added to the exponent,
+// and the sum is taken of pairs of rounded weights.
+#include "int8_attention.h"
+
+namespace wq {
+
+namespace {
+
+constexpr int kWaves = 4;
+
+// Below this ratio of a block's scale to the largest, and where tokens are hidden, the weights are summed before it is multiplied in: they
+// would lose their last bits, and hidden ones are picked out by hand.
+constexpr float kLeastRatio = 0x1p-6f;
+
+template <int TYPE, int D, int RT, int TOKENS>
+__global__ __launch_bounds__(64 * kWaves, 2) void int8_attention_many_kernel(AttentionArgs a, int items) {
+    typedef typename Element<TYPE>::type T;
+    typedef T V8 __attribute__((ext_vector_type(8)));
+    constexpr int kDims = D / 16, kParts = TOKENS / 16, kLane = TOKENS / 4;   // kLane: neighbouring tokens whose scores a lane holds
+    constexpr int kPieces = TOKENS * D / 16 / (64 * kWaves);                  // 16-byte pieces of keys that a thread brings, and of values
+    constexpr int kKeyChunks = D / 8, kValueChunks = TOKENS / 8;              // of 8 float16 in a row in LDS
+    constexpr int kKeyMask = kKeyChunks < 16 ? kKeyChunks - 1 : 15;
+    static_assert(kPieces >= 1 && kLane % 8 == 0, "a tile is shared out evenly");
+    // keys: row 16 part + r holds token kLane (r / 4) + 4 part + r % 4, chunk c at c ^ (row & 15) or fewer bits of it; values:
+    // row d, chunk c at c ^ (d & 7)
+    __shared__ v8h keys[2][TOKENS * kKeyChunks];
+    __shared__ v8h values[2][D * kValueChunks];
+    __shared__ float scales[2][2][kParts];   // of 16 tokens each: of keys, of values
+    __shared__ int bad[2][kParts];           // they lie in no block
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, quarter = lane >> 4;
+    // a head of keys to an XCD as far as there are eight, long rows of a sequence first
+    const int split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits, kv_head = rest % a.kv_heads, item = items - 1 - rest / a.kv_heads;
+    Tile t;
+    if (!tile_of(a, item, kv_head, t)) return;
+    const int first_step = split * t.per, last_step = min(t.steps, first_step + t.per);
+    if (split > 0 && first_step >= t.steps) return;
+    const bool alone = t.per >= t.steps;
+    const int begin = t.begin + first_step * kStep, tiles = max(last_step - first_step, 0) * (kStep / TOKENS);
+
+    // a lane's rows: columns of the scores' product, and of the result's
+    int low[RT], high[RT];
+    float to_exponent[RT];
+    v8h qs[RT][D / 32];
+    auto row_of = [&](int rt, bool& real, int& token, int& head) {
+        const int r = (wave * RT + rt) * 16 + row;
+        real = r < t.tokens * t.heads;
+        token = real ? r / t.heads : 0;
+        head = t.head0 + (real ? r % t.heads : 0);
+    };
+    int wave_low = 0x7fffffff, wave_high = 0, wave_low_all = 0, wave_high_all = 0x7fffffff;   // any row sees, every row sees
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        bool real;
+        int token, head;
+        row_of(rt, real, token, head);
+        visible(a, t.sequence.length - t.sequence.count + t.token0 + token, t.sequence.length, low[rt], high[rt]);
+        if (!real) high[rt] = 0;
+        wave_low = min(wave_low, real ? low[rt] : 0x7fffffff);
+        wave_high = max(wave_high, high[rt]);
+        wave_low_all = max(wave_low_all, real ? low[rt] : 0);
+        wave_high_all = min(wave_high_all, real ? high[rt] : 0x7fffffff);
+        const T* const query = static_cast<const T*>(a.q) + (long long)(t.sequence.first + t.token0 + token) * a.q_stride + (long long)head * D + 8 * quarter;
+        V8 raw[D / 32];
+        float most = 0.0f;
+#pragma unroll
+        for (int f = 0; f < D / 32; ++f) {
+            raw[f] = load_unaligned<V8, 2>(query + 32 * f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf((float)raw[f][j]));
+        }
+        most = fmaxf(most, __shfl_xor(most, 16));
+        most = fmaxf(most, __shfl_xor(most, 32));
+        float up = 1.0f, down = 1.0f;
+        if (TYPE == WQ_BF16) half_powers(most, up, down);
+        up *= a.sign;
+#pragma unroll
+        for (int f = 0; f < D / 32; ++f)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) qs[rt][f][j] = (_Float16)((float)raw[f][j] * up);
+        to_exponent[rt] = a.scale_log2 * down;
+    }
+#pragma unroll
+    for (int step = 8; step > 0; step >>= 1) {
+        wave_low = min(wave_low, __shfl_xor(wave_low, step));
+        wave_high = max(wave_high, __shfl_xor(wave_high, step));
+        wave_low_all = max(wave_low_all, __shfl_xor(wave_low_all, step));
+        wave_high_all = min(wave_high_all, __shfl_xor(wave_high_all, step));
+    }
+    wave_low = __builtin_amdgcn_readfirstlane(wave_low); wave_high = __builtin_amdgcn_readfirstlane(wave_high);
+    wave_low_all = __builtin_amdgcn_readfirstlane(wave_low_all); wave_high_all = __builtin_amdgcn_readfirstlane(wave_high_all);
+
+    const Batch& b = a.batch;
+    const int32_t* const table = b.table + (long long)t.s * b.width;
+    const int block_mask = (1 << b.shift) - 1, last_block = (t.sequence.length - 1) >> b.shift;
+    const long long block_bytes = (long long)D << b.shift;
+
+    // the pages of a tile's pieces come a tile earlier than the pieces
+    struct Pages { int key[kPieces], value[kPieces], own; };
+    struct Pieces { v4u key[kPieces], value[kPieces]; float k_scale, v_scale; int bad; };
+    auto key_token = [&](int i) { return (i * 64 * kWaves + (int)threadIdx.x) / (D / 16); };
+    auto value_group = [&](int i) { return (i * 64 * kWaves + (int)threadIdx.x) % kParts; };
+    auto page_at = [&](int token) { return table[min(token >> b.shift, last_block)]; };
+    auto find = [&](Pages& p, int tile) {
+        const int token0 = begin + tile * TOKENS;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            p.key[i] = page_at(token0 + key_token(i));
+            p.value[i] = page_at(token0 + 16 * value_group(i));
+        }
+        p.own = page_at(token0 + 16 * (threadIdx.x & (kParts - 1)));
+    };
+    auto base_of = [&](int page) { return ((long long)((unsigned)page < (unsigned)b.blocks ? page : 0) * a.kv_heads + kv_head); };
+    auto load = [&](Pieces& l, const Pages& p, int tile) {
+        const int token0 = begin + tile * TOKENS;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int piece = i * 64 * kWaves + threadIdx.x;
+            l.key[i] = *reinterpret_cast<const v4u*>(a.k + base_of(p.key[i]) * block_bytes + ((token0 + key_token(i)) & block_mask) * D + piece % (D / 16) * 16);
+            l.value[i] = *reinterpret_cast<const v4u*>(a.v + base_of(p.value[i]) * block_bytes + ((long long)(piece / kParts) << b.shift) +
+                                                       ((token0 + 16 * value_group(i)) & block_mask));
+        }
+        l.bad = (unsigned)p.own >= (unsigned)b.blocks;
+        l.k_scale = a.k_scale[base_of(p.own)];
+        l.v_scale = a.v_scale[base_of(p.own)];
+    };
+    auto store = [&](const Pieces& l, int half) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int piece = i * 64 * kWaves + threadIdx.x, token = key_token(i);
+            const int r = 16 * ((token % kLane) >> 2) + 4 * (token / kLane) + (token & 3), chunk = piece % (D / 16) * 2;
+            keys[half][r * kKeyChunks + (chunk ^ (r & kKeyMask))] = codes_to_half(l.key[i][0], l.key[i][1]);
+            keys[half][r * kKeyChunks + ((chunk + 1) ^ (r & kKeyMask))] = codes_to_half(l.key[i][2], l.key[i][3]);
+            const int d = piece / kParts, v_chunk = value_group(i) * 2;
+            values[half][d * kValueChunks + (v_chunk ^ (d & (kValueChunks - 1)))] = codes_to_half(l.value[i][0], l.value[i][1]);
+            values[half][d * kValueChunks + ((v_chunk + 1) ^ (d & (kValueChunks - 1)))] = codes_to_half(l.value[i][2], l.value[i][3]);
+        }
+        if (threadIdx.x < kParts) {
+            scales[half][0][threadIdx.x] = l.k_scale;
+            scales[half][1][threadIdx.x] = l.v_scale;
+            bad[half][threadIdx.x] = l.bad;
+        }
+    };
+
+    v4f out[RT][kDims] = {};
+    float largest[RT], lowered[RT], sum[RT], unit = 0.0f;   // unit: the scale in which `out` is held
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        largest[rt] = -INFINITY;
+        lowered[rt] = sum[rt] = 0.0f;
+    }
+
+    auto work = [&](int half, int token_first) {
+        const int token0 = token_first + kLane * quarter;   // the first of the lane's tokens
+        const int own = kLane * quarter / 16;               // their place among the scales
+        const bool hidden = bad[half][own];
+        const float k_scale = scales[half][0][own];
+        float v_scale = scales[half][1][own];
+        const bool masked = token_first < wave_low_all || token_first + TOKENS > wave_high_all || __any(hidden);
+        v4f scores[RT][kParts];
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) scores[rt][part] = v4f{};
+#pragma unroll
+            for (int f = 0; f < D / 32; ++f) {
+                const v8h k = keys[half][(16 * part + row) * kKeyChunks + ((4 * f + quarter) ^ (row & kKeyMask))];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) scores[rt][part] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qs[rt][f], scores[rt][part], 0, 0, 0);
+            }
+        }
+        if (masked) {
+            if (hidden || token0 >= wave_high || token0 + kLane <= wave_low) v_scale = 0.0f;   // whatever lies there
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int token = token0 + 4 * part + i;
+                        if (hidden || token < low[rt] || token >= high[rt]) scores[rt][part][i] = -INFINITY;
+                    }
+        }
+        float top[RT], factor[RT];
+        bool grown = v_scale > unit;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            factor[rt] = k_scale * to_exponent[rt];
+            float most = -INFINITY;
+#pragma unroll
+            for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) most = fmaxf(most, scores[rt][part][i]);
+            top[rt] = most == -INFINITY ? most : most * factor[rt];
+            grown = grown || top[rt] > largest[rt] + kSlack;
+        }
+        if (__any(grown)) {
+            float scale = fmaxf(v_scale, __shfl_xor(v_scale, 16));
+            scale = fmaxf(unit, fmaxf(scale, __shfl_xor(scale, 32)));
+            const float shrink = scale > 0.0f ? unit / scale : 0.0f;
+            unit = scale;
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                float most = fmaxf(top[rt], __shfl_xor(top[rt], 16));
+                most = fmaxf(most, __shfl_xor(most, 32));
+                const float now = fmaxf(largest[rt], most);
+                const float change = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(largest[rt] - now);
+                sum[rt] *= change;
+#pragma unroll
+                for (int d = 0; d < kDims; ++d) out[rt][d] *= change * shrink;
+                largest[rt] = now;
+                lowered[rt] = now == -INFINITY ? 0.0f : now - kRaise;
+            }
+        }
+        const float ratio = unit > 0.0f ? v_scale / unit : 0.0f;
+        v8h weights[RT][TOKENS / 32];
+        if (masked || __any(!(ratio >= kLeastRatio))) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float s = scores[rt][part][i];
+                        const float p = s == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(__builtin_fmaf(s, factor[rt], -lowered[rt]));
+                        sum[rt] += p;
+                        weights[rt][part >> 1][4 * (part & 1) + i] = (_Float16)(p > 0.0f || p != p ? p * ratio : 0.0f);
+                    }
+        } else {
+            const float raise = __builtin_amdgcn_logf(ratio), back = 1.0f / ratio;
+            const v2h one = {(_Float16)1.0f, (_Float16)1.0f};
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const float lower = raise - lowered[rt];
+                float own_sum = 0.0f;
+#pragma unroll
+                for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                    for (int i = 0; i < 4; i += 2) {
+                        v2h w;
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) w[j] = (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(scores[rt][part][i + j], factor[rt], lower));
+                        own_sum = __builtin_amdgcn_fdot2(w, one, own_sum, false);
+                        weights[rt][part >> 1][4 * (part & 1) + i] = w[0];
+                        weights[rt][part >> 1][4 * (part & 1) + i + 1] = w[1];
+                    }
+                sum[rt] = __builtin_fmaf(own_sum, back, sum[rt]);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < TOKENS / 32; ++u)
+#pragma unroll
+            for (int d = 0; d < kDims; ++d) {
+                const v8h v = values[half][(16 * d + row) * kValueChunks + ((kLane / 8 * quarter + u) ^ (row & (kValueChunks - 1)))];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) out[rt][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, weights[rt][u], out[rt][d], 0, 0, 0);
+            }
+    };
+
+    if (tiles > 0) {
+        Pages pages;
+        Pieces pieces;
+        find(pages, 0);
+        load(pieces, pages, 0);
+        find(pages, min(1, tiles - 1));
+        store(pieces, 0);
+        load(pieces, pages, min(1, tiles - 1));
+        find(pages, min(2, tiles - 1));
+        for (int tile = 0; tile < tiles; ++tile) {
+            __syncthreads();   // this tile is there, the other half has been read
+            if (tile + 1 < tiles) {
+                store(pieces, (tile + 1) & 1);
+                load(pieces, pages, min(tile + 2, tiles - 1));
+                find(pages, min(tile + 3, tiles - 1));
+            }
+            const int token_first = begin + tile * TOKENS;
+            if (token_first < wave_high && token_first + TOKENS > wave_low) work(tile & 1, token_first);
+        }
+    }
+
+    float* const partial = a.partial + (((long long)item * a.kv_heads + kv_head) * a.splits + split) * ((long long)a.tile_rows * (D + 2));
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        bool real;
+        int token, head;
+        row_of(rt, real, token, head);
+        float total = sum[rt] + __shfl_xor(sum[rt], 16);
+        total += __shfl_xor(total, 32);
+        if (!real) continue;
+        const float over = alone ? (total == 0.0f ? 0.0f : unit / total) : unit;   // NaN stays NaN
+        const int r = (wave * RT + rt) * 16 + row;
+        if (!alone && quarter == 0) {
+            partial[a.tile_rows * D + 2 * r] = largest[rt];
+            partial[a.tile_rows * D + 2 * r + 1] = total;
+        }
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) {
+            const v4f v = out[rt][d] * over;
+            if (alone) store4<TYPE>(a.out, (long long)(t.sequence.first + t.token0 + token) * a.out_stride + (long long)head * D + 16 * d + 4 * quarter, v);
+            else *reinterpret_cast<v4f*>(partial + (long long)r * D + 16 * d + 4 * quarter) = v;
+        }
+    }
+}
+
+template <int TYPE, int D, int RT, int TOKENS>
+hipError_t launch(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) {
+    static_assert(64 * RT == many_rows(D), "rows of a workgroup");
+    int8_attention_many_kernel<TYPE, D, RT, TOKENS><<<(unsigned)(p.items * a.kv_heads * p.splits), 64 * kWaves, 0, s>>>(a, (int)p.items);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attention_many(const AttentionArgs& a, const AttentionPlan& p, int type, int head_dim, hipStream_t s) {
+    if (type == WQ_F16)
+        return head_dim == 64 ? launch<WQ_F16, 64, 3, 64>(a, p, s) : head_dim == 128 ? launch<WQ_F16, 128, 3, 32>(a, p, s) : launch<WQ_F16, 256, 1, 32>(a, p, s);
+    return head_dim == 64 ? launch<WQ_BF16, 64, 3, 64>(a, p, s) : head_dim == 128 ? launch<WQ_BF16, 128, 3, 32>(a, p, s) : launch<WQ_BF16, 256, 1, 32>(a, p, s);
+}
+
+}  // namespace wq

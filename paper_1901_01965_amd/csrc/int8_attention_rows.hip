@@ -19,38 +19,6 @@ namespace wq {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kStep = 64;        // tokens a wave takes at a time
-constexpr int kLeastSteps = 4;   // of a part of a sequence: one for each wave
-
-// A tile's rows and tokens.
-struct Tile {
-    Sequence sequence;
-    int s, token0, tokens;      // its first row in the sequence, rows
-    int head0, heads;           // first head of queries, heads
-    int begin, steps, per;      // tokens from `begin` on in steps of kStep, of which a part has `per`
-    int low, high;              // tokens that any row sees
-    int low_all, high_all;      // tokens that every row sees, unless low_all >= high_all
-};
-
-__device__ inline bool tile_of(const AttentionArgs& a, int tokens_shift, int head_tiles, int item, int y, Tile& t) {
-    const Batch& b = a.batch;
-    t.s = b.starts ? sequence_of_item(b, item, tokens_shift, 1) : item;
-    t.sequence = sequence_of(b, t.s);
-    t.token0 = b.starts ? (item - item_base(b, t.s, tokens_shift, 1)) << tokens_shift : 0;
-    if (t.token0 < 0 || t.token0 >= t.sequence.count) return false;
-    t.tokens = min(1 << tokens_shift, t.sequence.count - t.token0);
-    const int tile = y % head_tiles;
-    t.head0 = y / head_tiles * a.group + 16 * tile;
-    t.heads = min(a.group - 16 * tile, 16);
-    const int position = t.sequence.length - t.sequence.count + t.token0;
-    visible(a, position, t.sequence.length, t.low, t.high_all);
-    visible(a, position + t.tokens - 1, t.sequence.length, t.low_all, t.high);
-    t.begin = t.low & ~(kStep - 1);
-    t.steps = max(ceil_div(t.high - t.begin, kStep), 0);
-    t.per = ceil_div(t.steps, min(a.splits, max(t.steps / kLeastSteps, 1)));
-    return true;
-}
-
 template <int D>
 struct Loads {
     v4u k[4][D / 64];
@@ -60,7 +28,7 @@ struct Loads {
 };
 
 template <int TYPE, int D>
-__global__ __launch_bounds__(64 * kWaves) void int8_attention_kernel(AttentionArgs a, int tokens_shift, int head_tiles) {
+__global__ __launch_bounds__(64 * kWaves) void int8_attention_kernel(AttentionArgs a) {
     typedef typename Element<TYPE>::type T;
     constexpr int kDims = D / 16;   // 16-row tiles of the result
     constexpr int kRound = kDims < 8 ? kDims : 8;   // of which the waves join at a time
@@ -70,7 +38,7 @@ __global__ __launch_bounds__(64 * kWaves) void int8_attention_kernel(AttentionAr
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int split = blockIdx.x % a.splits;
     Tile t;
-    if (!tile_of(a, tokens_shift, head_tiles, blockIdx.x / a.splits, blockIdx.y, t)) return;
+    if (!tile_of(a, blockIdx.x / a.splits, blockIdx.y, t)) return;
     const int first_step = split * t.per, last_step = min(t.steps, first_step + t.per);
     if (split > 0 && first_step >= t.steps) return;
     const bool alone = t.per >= t.steps;
@@ -98,6 +66,7 @@ __global__ __launch_bounds__(64 * kWaves) void int8_attention_kernel(AttentionAr
     most = fmaxf(most, __shfl_xor(most, 32));
     float up = 1.0f, down = 1.0f;
     if (TYPE == WQ_BF16) half_powers(most, up, down);
+    up *= a.sign;
     v8h qs[D / 32];
 #pragma unroll
     for (int f = 0; f < D / 32; ++f)
@@ -107,7 +76,7 @@ __global__ __launch_bounds__(64 * kWaves) void int8_attention_kernel(AttentionAr
 
     const Batch& b = a.batch;
     const int32_t* const table = b.table + (long long)t.s * b.width;
-    const int kv_head = blockIdx.y / head_tiles, block_mask = (1 << b.shift) - 1, last_block = (t.sequence.length - 1) >> b.shift;
+    const int kv_head = blockIdx.y / a.head_tiles, block_mask = (1 << b.shift) - 1, last_block = (t.sequence.length - 1) >> b.shift;
     const long long block_bytes = (long long)D << b.shift;
 
     auto load = [&](Loads<D>& l, int step) {
@@ -245,67 +214,13 @@ __global__ __launch_bounds__(64 * kWaves) void int8_attention_kernel(AttentionAr
     }
 }
 
-// Joins the parts of a row: one workgroup per row, its threads share the parts out.
-template <int TYPE, int D>
-__global__ __launch_bounds__(256) void int8_attention_join_kernel(AttentionArgs a, int tokens_shift, int head_tiles) {
-    constexpr int kAcross = D / 4, kDown = 256 / kAcross;
-    __shared__ v4f sums[kDown][kAcross];
-    __shared__ float totals[kDown];
-    Tile t;
-    if (!tile_of(a, tokens_shift, head_tiles, blockIdx.x / 16, blockIdx.y, t)) return;
-    const int row = blockIdx.x & 15;
-    if (row >= t.tokens * t.heads || t.per >= t.steps) return;
-    const int parts = ceil_div(t.steps, t.per), across = threadIdx.x % kAcross, down = threadIdx.x / kAcross;
-    const long long each = 16 * (D + 2);
-    const float* const partial = a.partial + ((long long)(blockIdx.x / 16) * gridDim.y + blockIdx.y) * a.splits * each;
-    float all = -INFINITY;
-    for (int p = 0; p < parts; ++p) all = fmaxf(all, partial[p * each + 16 * D + 2 * row]);
-    v4f r = {};
-    float total = 0.0f;
-    for (int p = down; p < parts; p += kDown) {
-        const float* const part = partial + p * each;
-        const float largest = part[16 * D + 2 * row];
-        const float factor = largest == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(largest - all);
-        if (largest != -INFINITY) total += part[16 * D + 2 * row + 1] * factor;
-        r += *reinterpret_cast<const v4f*>(part + row * D + 4 * across) * factor;
-    }
-    sums[down][across] = r;
-    if (across == 0) totals[down] = total;
-    __syncthreads();
-    if (down != 0) return;
-    for (int i = 1; i < kDown; ++i) {
-        r += sums[i][across];
-        total += totals[i];
-    }
-    const float over = total == 0.0f ? 0.0f : 1.0f / total;
-    const long long row_at = (long long)(t.sequence.first + t.token0 + row / t.heads);
-    store4<TYPE>(a.out, row_at * a.out_stride + (long long)(t.head0 + row % t.heads) * D + 4 * across, r * over);
-}
-
 template <int TYPE, int D>
 hipError_t launch(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) {
-    const unsigned y = a.kv_heads * p.head_tiles;
-    int8_attention_kernel<TYPE, D><<<dim3((unsigned)(p.items * p.splits), y), 64 * kWaves, 0, s>>>(a, p.tokens_shift, p.head_tiles);
-    if (hipError_t e = hipGetLastError()) return e;
-    if (p.splits > 1) int8_attention_join_kernel<TYPE, D><<<dim3((unsigned)(p.items * 16), y), 256, 0, s>>>(a, p.tokens_shift, p.head_tiles);
+    int8_attention_kernel<TYPE, D><<<dim3((unsigned)(p.items * p.splits), a.kv_heads * a.head_tiles), 64 * kWaves, 0, s>>>(a);
     return hipGetLastError();
 }
 
 }  // namespace
-
-AttentionPlan plan_attention(int rows, int heads, int kv_heads, int head_dim, int block, int width, int sequences, bool has_starts) {
-    AttentionPlan p;
-    const int group = heads / kv_heads;
-    p.head_tiles = ceil_div(group, 16);
-    p.tokens_shift = 0;
-    while (has_starts && (2 << p.tokens_shift) * group <= 16) ++p.tokens_shift;
-    p.items = has_starts ? item_count(rows, sequences, p.tokens_shift, 1) : sequences;
-    const long long tiles = p.items * kv_heads * p.head_tiles;
-    const long long most = max((long long)width * block / (kStep * kLeastSteps), 1ll);
-    p.splits = (int)min(max((8ll * kComputeUnits + tiles - 1) / tiles, 1ll), most);
-    p.workspace = p.splits > 1 ? (size_t)tiles * p.splits * 16 * (head_dim + 2) * sizeof(float) : 0;
-    return p;
-}
 
 hipError_t launch_attention_rows(const AttentionArgs& a, const AttentionPlan& p, int type, int head_dim, hipStream_t s) {
     if (type == WQ_F16) return head_dim == 64 ? launch<WQ_F16, 64>(a, p, s) : head_dim == 128 ? launch<WQ_F16, 128>(a, p, s) : launch<WQ_F16, 256>(a, p, s);
@@ -313,44 +228,3 @@ hipError_t launch_attention_rows(const AttentionArgs& a, const AttentionPlan& p,
 }
 
 }  // namespace wq
-
-using namespace wq;
-
-extern "C" {
-
-size_t int8_cache_attention_workspace_bytes(int rows, int heads, int kv_heads, int head_dim, int block, int table_width,
-                                            int sequences, int has_starts) {
-    if (rows <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || table_width <= 0 || sequences <= 0) return 0;
-    if ((head_dim != 64 && head_dim != 128 && head_dim != 256) || (block != 16 && block != 32 && block != 64 && block != 128)) return 0;
-    return plan_attention(rows, heads, kv_heads, head_dim, block, table_width, sequences, has_starts != 0).workspace;
-}
-
-int int8_cache_attention(const void* q_dev, long long q_stride, int type, int rows, int heads, const int8_t* cache_k_dev,
-                         const int8_t* cache_v_dev, const float* k_scale_dev, const float* v_scale_dev, int blocks, int kv_heads,
-                         int head_dim, int block, const int32_t* table_dev, int table_width, int sequences,
-                         const int32_t* lengths_dev, const int32_t* starts_dev, float scale, int causal, int window, void* out_dev,
-                         long long out_stride, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
-    const CacheArgs c = {cache_k_dev, cache_v_dev, k_scale_dev, v_scale_dev, blocks, kv_heads, head_dim, block};
-    if (int st = check_cache(c)) return st;
-    bool empty;
-    if (int st = check_batch(rows, table_dev, table_width, sequences, lengths_dev, starts_dev, block, empty)) return st;
-    if (!is_half(type) || heads <= 0 || heads % kv_heads || window < 0 || (window > 0 && !causal)) return WG_EINVAL;
-    if (!(scale - scale == 0.0f)) return WG_EINVAL;   // infinite or NaN
-    if (heads > 8192) return WG_EUNSUPPORTED;
-    if (q_stride < (long long)heads * head_dim || out_stride < (long long)heads * head_dim) return WG_EINVAL;
-    if (empty) return WG_OK;
-    if (!q_dev || !out_dev || !aligned(q_dev, 2) || !aligned(out_dev, 2)) return WG_EINVAL;
-    const AttentionPlan p = plan_attention(rows, heads, kv_heads, head_dim, block, table_width, sequences, starts_dev != nullptr);
-    if (p.items * max(p.splits, 16) > kMostItems) return WG_EUNSUPPORTED;
-    if (p.workspace > 0) {
-        if (!workspace_dev || !aligned(workspace_dev, 256)) return WG_EINVAL;
-        if (workspace_bytes < p.workspace) return WG_ESMALLBUF;
-    }
-    const AttentionArgs a = {q_dev, q_stride, out_dev, out_stride, cache_k_dev, cache_v_dev, k_scale_dev, v_scale_dev,
-                             static_cast<float*>(workspace_dev),
-                             {table_dev, lengths_dev, starts_dev, table_width, sequences, rows, blocks, block_shift(block)},
-                             kv_heads, heads / kv_heads, causal != 0, window, p.splits, scale * 1.44269504088896340736f};
-    return status_of(launch_attention_rows(a, p, type, head_dim, static_cast<hipStream_t>(hip_stream)));
-}
-
-}  // extern "C"

@@ -78,10 +78,10 @@ __global__ __launch_bounds__(kThreads) void int8_append_kernel(AppendArgs a) {
 
     const Batch& b = a.batch;
     const int item = blockIdx.x, head = blockIdx.y, is_v = blockIdx.z, P = 1 << b.shift;
-    const int s = b.starts ? sequence_of_item(b, item, b.shift, 2) : item;
+    const int s = b.starts ? sequence_of_item(b, item, P, 2) : item;
     const Sequence q = sequence_of(b, s);
     const long long base = (long long)q.length - q.count;   // position of the first row
-    const int local = b.starts ? item - item_base(b, s, b.shift, 2) : 0;
+    const int local = b.starts ? item - item_base(b, s, P, 2) : 0;
     if (local < 0 || q.count <= 0 || q.length <= 0) return;
     const int index = (int)(max(base, 0ll) >> b.shift) + local;
     if (index > (q.length - 1) >> b.shift) return;
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(kThreads) void int8_append_kernel(AppendArgs a) {
 
 template <int TYPE, int D>
 hipError_t append(const AppendArgs& a, hipStream_t s) {
-    const long long items = a.batch.starts ? item_count(a.batch.rows, a.batch.sequences, a.batch.shift, 2) : a.batch.sequences;
+    const long long items = a.batch.starts ? item_count(a.batch.rows, a.batch.sequences, 1 << a.batch.shift, 2) : a.batch.sequences;
     int8_append_kernel<TYPE, D><<<dim3((unsigned)items, a.kv_heads, 2), kThreads, 0, s>>>(a);
     return hipGetLastError();
 }
@@ -269,7 +269,7 @@ int int8_cache_append(const void* k_dev, long long k_stride, const void* v_dev, 
     if (empty) return WG_OK;
     if (!k_dev || !v_dev || !aligned(k_dev, 2) || !aligned(v_dev, 2)) return WG_EINVAL;
     const Batch b = {table_dev, lengths_dev, starts_dev, table_width, sequences, rows, blocks, block_shift(block)};
-    if (item_count(rows, sequences, b.shift, 2) > kMostItems) return WG_EUNSUPPORTED;
+    if (item_count(rows, sequences, block, 2) > kMostItems) return WG_EUNSUPPORTED;
     const AppendArgs a = {{k_dev, v_dev}, {k_stride, v_stride}, {cache_k_dev, cache_v_dev}, {k_scale_dev, v_scale_dev}, b, kv_heads};
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
     if (type == WQ_F16)

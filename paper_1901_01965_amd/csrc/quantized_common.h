@@ -76,19 +76,19 @@ __device__ inline Sequence sequence_of(const Batch& b, int s) {
     return {first, max(start_of(b, s + 1) - first, 0), min(max(b.lengths[s], 0), most)};
 }
 
-// Work items are dealt to sequences without a table of their sums: sequence s owns the items base(s) .. base(s + 1) - 1 with
-// base(s) = floor(start(s) / unit) + extra * s, which are at least count / unit, rounded up, plus extra - 1.  Finds the sequence of
-// an item; starts that fall are read as a clamped search finds them.
-__device__ inline int item_base(const Batch& b, int s, int unit_shift, int extra) { return (start_of(b, s) >> unit_shift) + extra * s; }
-__device__ inline int sequence_of_item(const Batch& b, int item, int unit_shift, int extra) {
+// Work items of `unit` rows are dealt to sequences without a table of their sums: sequence s owns the items base(s) ..
+// base(s + 1) - 1 with base(s) = floor(start(s) / unit) + extra * s, which are at least count / unit, rounded up, plus extra - 1.
+// Finds the sequence of an item; starts that fall are read as a clamped search finds them.
+__device__ inline int item_base(const Batch& b, int s, int unit, int extra) { return start_of(b, s) / unit + extra * s; }
+__device__ inline int sequence_of_item(const Batch& b, int item, int unit, int extra) {
     int low = 0, high = b.sequences - 1;
     while (low < high) {
         const int middle = (low + high + 1) >> 1;
-        if (item_base(b, middle, unit_shift, extra) <= item) low = middle;
+        if (item_base(b, middle, unit, extra) <= item) low = middle;
         else high = middle - 1;
     }
     return low;
 }
-inline long long item_count(int rows, int sequences, int unit_shift, int extra) { return (rows >> unit_shift) + (long long)extra * sequences; }
+inline long long item_count(int rows, int sequences, int unit, int extra) { return rows / unit + (long long)extra * sequences; }
 
 }  // namespace wq

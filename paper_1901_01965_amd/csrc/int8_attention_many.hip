@@ -27,12 +27,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int8_attention_many_kernel(Att
     constexpr int kKeyChunks = D / 8, kValueChunks = TOKENS / 8;              // of 8 float16 in a row in LDS
     constexpr int kKeyMask = kKeyChunks < 16 ? kKeyChunks - 1 : 15;
     static_assert(kPieces >= 1 && kLane % 8 == 0, "a tile is shared out evenly");
-    // keys: row 16 part + r holds token kLane (r / 4) + 4 part + r % 4, chunk c at c ^ (row & 15) or fewer bits of it; values:
-    // row d, chunk c at c ^ (d & 7)
+    // keys: row 16 part + r holds token kLane (r / 4) + 4 part + r % 4; chunks lie so that no two of eight rows' share banks
     __shared__ v8h keys[2][TOKENS * kKeyChunks];
     __shared__ v8h values[2][D * kValueChunks];
-    __shared__ float scales[2][2][kParts];   // of 16 tokens each: of keys, of values
-    __shared__ int bad[2][kParts];           // they lie in no block
+    auto key_at = [](int r, int chunk) { return r * kKeyChunks + (chunk ^ (r & kKeyMask)); };
+    auto value_at = [](int d, int chunk) {
+        if (kValueChunks == 8) return d * 8 + (chunk ^ (d & 7));
+        return (d >> 2) * 16 + (((d & 3) ^ ((d >> 2) & 3)) * 4 + (chunk ^ (d & 3)));   // four rows to 256 bytes
+    };
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, quarter = lane >> 4;
     // a head of keys to an XCD as far as there are eight, long rows of a sequence first
@@ -101,67 +103,66 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int8_attention_many_kernel(Att
     const int block_mask = (1 << b.shift) - 1, last_block = (t.sequence.length - 1) >> b.shift;
     const long long block_bytes = (long long)D << b.shift;
 
-    // the pages of a tile's pieces come a tile earlier than the pieces
-    struct Pages { int key[kPieces], value[kPieces], own; };
-    struct Pieces { v4u key[kPieces], value[kPieces]; float k_scale, v_scale; int bad; };
-    auto key_token = [&](int i) { return (i * 64 * kWaves + (int)threadIdx.x) / (D / 16); };
-    auto value_group = [&](int i) { return (i * 64 * kWaves + (int)threadIdx.x) % kParts; };
-    auto page_at = [&](int token) { return table[min(token >> b.shift, last_block)]; };
-    auto find = [&](Pages& p, int tile) {
-        const int token0 = begin + tile * TOKENS;
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            p.key[i] = page_at(token0 + key_token(i));
-            p.value[i] = page_at(token0 + 16 * value_group(i));
-        }
-        p.own = page_at(token0 + 16 * (threadIdx.x & (kParts - 1)));
+    // Where a tile's tokens lie, 16 of them in one block each, is asked for a tile ahead of the codes; a lane asks for those tokens whose
+    // scores it will hold.  What a wave brings of the keys lies in one block, and of the values as well: their places are scalars.  (They
+    // are not loaded as such: scalar loads on their way would be waited for with every read of LDS.)
+    const int own = kLane * quarter / 16;   // which 16 tokens
+    struct Pieces {
+        v4u key[kPieces], value[kPieces];
+        float k_scale, v_scale;
+        int hidden;   // they lie in no block
     };
-    auto base_of = [&](int page) { return ((long long)((unsigned)page < (unsigned)b.blocks ? page : 0) * a.kv_heads + kv_head); };
-    auto load = [&](Pieces& l, const Pages& p, int tile) {
+    auto find = [&](int tile) { return table[min((begin + tile * TOKENS + 16 * own) >> b.shift, last_block)]; };
+    auto load = [&](Pieces& l, int page, int tile) {
         const int token0 = begin + tile * TOKENS;
+        l.hidden = (unsigned)page >= (unsigned)b.blocks;
+        const int at = l.hidden ? 0 : page;
+        const long long mine = (long long)at * a.kv_heads + kv_head;
+        l.k_scale = a.k_scale[mine];
+        l.v_scale = a.v_scale[mine];
+        long long base[kParts];
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) base[i] = (long long)__builtin_amdgcn_readlane(at, 16 * (16 / kLane) * i) * a.kv_heads + kv_head;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            const int piece = i * 64 * kWaves + threadIdx.x;
-            l.key[i] = *reinterpret_cast<const v4u*>(a.k + base_of(p.key[i]) * block_bytes + ((token0 + key_token(i)) & block_mask) * D + piece % (D / 16) * 16);
-            l.value[i] = *reinterpret_cast<const v4u*>(a.v + base_of(p.value[i]) * block_bytes + ((long long)(piece / kParts) << b.shift) +
-                                                       ((token0 + 16 * value_group(i)) & block_mask));
+            const int key_token = (i * kWaves + wave) * (64 / (D / 16)), slot = i * kWaves + wave, group = slot / (D / 64);
+            long long key_base = base[0], value_base = base[0];
+#pragma unroll
+            for (int j = 1; j < kParts; ++j) {
+                key_base = key_token >= 16 * j ? base[j] : key_base;
+                value_base = group >= j ? base[j] : value_base;
+            }
+            l.key[i] = *reinterpret_cast<const v4u*>(a.k + key_base * block_bytes + ((token0 + key_token) & block_mask) * D + 16 * lane);
+            l.value[i] = *reinterpret_cast<const v4u*>(a.v + value_base * block_bytes + ((token0 + 16 * group) & block_mask) +
+                                                       (((slot % (D / 64)) * 64 + lane) << b.shift));
         }
-        l.bad = (unsigned)p.own >= (unsigned)b.blocks;
-        l.k_scale = a.k_scale[base_of(p.own)];
-        l.v_scale = a.v_scale[base_of(p.own)];
     };
     auto store = [&](const Pieces& l, int half) {
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            const int piece = i * 64 * kWaves + threadIdx.x, token = key_token(i);
-            const int r = 16 * ((token % kLane) >> 2) + 4 * (token / kLane) + (token & 3), chunk = piece % (D / 16) * 2;
-            keys[half][r * kKeyChunks + (chunk ^ (r & kKeyMask))] = codes_to_half(l.key[i][0], l.key[i][1]);
-            keys[half][r * kKeyChunks + ((chunk + 1) ^ (r & kKeyMask))] = codes_to_half(l.key[i][2], l.key[i][3]);
-            const int d = piece / kParts, v_chunk = value_group(i) * 2;
-            values[half][d * kValueChunks + (v_chunk ^ (d & (kValueChunks - 1)))] = codes_to_half(l.value[i][0], l.value[i][1]);
-            values[half][d * kValueChunks + ((v_chunk + 1) ^ (d & (kValueChunks - 1)))] = codes_to_half(l.value[i][2], l.value[i][3]);
-        }
-        if (threadIdx.x < kParts) {
-            scales[half][0][threadIdx.x] = l.k_scale;
-            scales[half][1][threadIdx.x] = l.v_scale;
-            bad[half][threadIdx.x] = l.bad;
+            const int token = (i * kWaves + wave) * (64 / (D / 16)) + lane / (D / 16), chunk = lane % (D / 16) * 2;
+            const int r = 16 * ((token % kLane) >> 2) + 4 * (token / kLane) + (token & 3);
+            keys[half][key_at(r, chunk)] = codes_to_half(l.key[i][0], l.key[i][1]);
+            keys[half][key_at(r, chunk + 1)] = codes_to_half(l.key[i][2], l.key[i][3]);
+            const int slot = i * kWaves + wave, group = slot / (D / 64), d = (slot % (D / 64)) * 64 + lane;
+            values[half][value_at(d, 2 * group)] = codes_to_half(l.value[i][0], l.value[i][1]);
+            values[half][value_at(d, 2 * group + 1)] = codes_to_half(l.value[i][2], l.value[i][3]);
         }
     };
 
     v4f out[RT][kDims] = {};
-    float largest[RT], lowered[RT], sum[RT], unit = 0.0f;   // unit: the scale in which `out` is held
+    float largest[RT], lowered[RT], sum[RT], unit = 0.0f, per_unit = 0.0f;   // unit: the scale in which `out` is held, and 1 / unit
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         largest[rt] = -INFINITY;
         lowered[rt] = sum[rt] = 0.0f;
     }
 
-    auto work = [&](int half, int token_first) {
+    auto work = [&](int half, int token_first, const Pieces& l) {
         const int token0 = token_first + kLane * quarter;   // the first of the lane's tokens
-        const int own = kLane * quarter / 16;               // their place among the scales
-        const bool hidden = bad[half][own];
-        const float k_scale = scales[half][0][own];
-        float v_scale = scales[half][1][own];
+        const float k_scale = l.k_scale;
+        float v_scale = l.v_scale;
+        const bool hidden = l.hidden;
         const bool masked = token_first < wave_low_all || token_first + TOKENS > wave_high_all || __any(hidden);
         v4f scores[RT][kParts];
 #pragma unroll
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int8_attention_many_kernel(Att
             for (int rt = 0; rt < RT; ++rt) scores[rt][part] = v4f{};
 #pragma unroll
             for (int f = 0; f < D / 32; ++f) {
-                const v8h k = keys[half][(16 * part + row) * kKeyChunks + ((4 * f + quarter) ^ (row & kKeyMask))];
+                const v8h k = keys[half][key_at(16 * part + row, 4 * f + quarter)];
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) scores[rt][part] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qs[rt][f], scores[rt][part], 0, 0, 0);
             }
@@ -205,6 +206,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int8_attention_many_kernel(Att
             scale = fmaxf(unit, fmaxf(scale, __shfl_xor(scale, 32)));
             const float shrink = scale > 0.0f ? unit / scale : 0.0f;
             unit = scale;
+            per_unit = unit > 0x1p-100f ? 1.0f / unit : 0.0f;   // without it every ratio takes the longer way below
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 float most = fmaxf(top[rt], __shfl_xor(top[rt], 16));
@@ -218,9 +220,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int8_attention_many_kernel(Att
                 lowered[rt] = now == -INFINITY ? 0.0f : now - kRaise;
             }
         }
-        const float ratio = unit > 0.0f ? v_scale / unit : 0.0f;
+        float ratio = v_scale * per_unit;
         v8h weights[RT][TOKENS / 32];
         if (masked || __any(!(ratio >= kLeastRatio))) {
+            ratio = unit > 0.0f ? v_scale / unit : 0.0f;
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -233,7 +236,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int8_attention_many_kernel(Att
                         weights[rt][part >> 1][4 * (part & 1) + i] = (_Float16)(p > 0.0f || p != p ? p * ratio : 0.0f);
                     }
         } else {
-            const float raise = __builtin_amdgcn_logf(ratio), back = 1.0f / ratio;
+            const float raise = __builtin_amdgcn_logf(ratio), back = __builtin_amdgcn_rcpf(ratio);
             const v2h one = {(_Float16)1.0f, (_Float16)1.0f};
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
@@ -257,30 +260,27 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int8_attention_many_kernel(Att
         for (int u = 0; u < TOKENS / 32; ++u)
 #pragma unroll
             for (int d = 0; d < kDims; ++d) {
-                const v8h v = values[half][(16 * d + row) * kValueChunks + ((kLane / 8 * quarter + u) ^ (row & (kValueChunks - 1)))];
+                const v8h v = values[half][value_at(16 * d + row, kLane / 8 * quarter + u)];
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) out[rt][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, weights[rt][u], out[rt][d], 0, 0, 0);
             }
     };
 
     if (tiles > 0) {
-        Pages pages;
-        Pieces pieces;
-        find(pages, 0);
-        load(pieces, pages, 0);
-        find(pages, min(1, tiles - 1));
-        store(pieces, 0);
-        load(pieces, pages, min(1, tiles - 1));
-        find(pages, min(2, tiles - 1));
+        Pieces now, next;
+        load(next, find(0), 0);
+        int page = find(min(1, tiles - 1));
         for (int tile = 0; tile < tiles; ++tile) {
-            __syncthreads();   // this tile is there, the other half has been read
+            // a tile is stored into the half that was read before the last barrier
+            now = next;
+            store(now, tile & 1);
             if (tile + 1 < tiles) {
-                store(pieces, (tile + 1) & 1);
-                load(pieces, pages, min(tile + 2, tiles - 1));
-                find(pages, min(tile + 3, tiles - 1));
+                load(next, page, tile + 1);
+                page = find(min(tile + 2, tiles - 1));
             }
+            __syncthreads();
             const int token_first = begin + tile * TOKENS;
-            if (token_first < wave_high && token_first + TOKENS > wave_low) work(tile & 1, token_first);
+            if (token_first < wave_high && token_first + TOKENS > wave_low) work(tile & 1, token_first, now);
         }
     }
 

@@ -93,7 +93,7 @@ struct AttentionPlan {
 };
 
 // Rows of a workgroup of the kernel for many rows.
-constexpr int many_rows(int head_dim) { return head_dim == 256 ? 64 : 192; }
+constexpr int many_rows(int head_dim) { return head_dim == 256 ? 64 : 128; }
 
 hipError_t launch_attention_rows(const AttentionArgs& a, const AttentionPlan& p, int type, int head_dim, hipStream_t s);
 hipError_t launch_attention_many(const AttentionArgs& a, const AttentionPlan& p, int type, int head_dim, hipStream_t s);

@@ -18,22 +18,22 @@ constexpr int kWaves = 4;
 // would lose their last bits, and hidden ones are picked out by hand.
 constexpr float kLeastRatio = 0x1p-6f;
 
-template <int TYPE, int D, int RT, int TOKENS>
-__global__ __launch_bounds__(64 * kWaves, 2) void int8_attention_many_kernel(AttentionArgs a, int items) {
+template <int TYPE, int D, int RT, int TOKENS, int WGS>
+__global__ __launch_bounds__(64 * kWaves, WGS) void int8_attention_many_kernel(AttentionArgs a, int items) {
     typedef typename Element<TYPE>::type T;
     typedef T V8 __attribute__((ext_vector_type(8)));
     constexpr int kDims = D / 16, kParts = TOKENS / 16, kLane = TOKENS / 4;   // kLane: neighbouring tokens whose scores a lane holds
     constexpr int kPieces = TOKENS * D / 16 / (64 * kWaves);                  // 16-byte pieces of keys that a thread brings, and of values
     constexpr int kKeyChunks = D / 8, kValueChunks = TOKENS / 8;              // of 8 float16 in a row in LDS
-    constexpr int kKeyMask = kKeyChunks < 16 ? kKeyChunks - 1 : 15;
     static_assert(kPieces >= 1 && kLane % 8 == 0, "a tile is shared out evenly");
     // keys: row 16 part + r holds token kLane (r / 4) + 4 part + r % 4; chunks lie so that no two of eight rows' share banks
     __shared__ v8h keys[2][TOKENS * kKeyChunks];
     __shared__ v8h values[2][D * kValueChunks];
-    auto key_at = [](int r, int chunk) { return r * kKeyChunks + (chunk ^ (r & kKeyMask)); };
+    // (reads of 16 bytes are served to lanes 0-3, 12-15, 20-23 and 24-27 at a time, and so on: eight rows of one quarter, eight of the next)
+    auto key_at = [](int r, int chunk) { return r * kKeyChunks + (chunk ^ (kKeyChunks == 8 ? (r >> 1 & 3) << 1 : r & 15)); };
     auto value_at = [](int d, int chunk) {
-        if (kValueChunks == 8) return d * 8 + (chunk ^ (d & 7));
-        return (d >> 2) * 16 + (((d & 3) ^ ((d >> 2) & 3)) * 4 + (chunk ^ (d & 3)));   // four rows to 256 bytes
+        const int line = d >> 2 & 3;   // of 256 bytes, where a row is 64
+        return d * kValueChunks + (chunk ^ (kValueChunks == 8 ? (d >> 1 & 1) | (d >> 2 & 1) << 2 : (line & 1) << 1 ^ (line >> 1) * 3));
     };
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, quarter = lane >> 4;
@@ -308,10 +308,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int8_attention_many_kernel(Att
     }
 }
 
-template <int TYPE, int D, int RT, int TOKENS>
+template <int TYPE, int D, int RT, int TOKENS, int WGS>
 hipError_t launch(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) {
     static_assert(64 * RT == many_rows(D), "rows of a workgroup");
-    int8_attention_many_kernel<TYPE, D, RT, TOKENS><<<(unsigned)(p.items * a.kv_heads * p.splits), 64 * kWaves, 0, s>>>(a, (int)p.items);
+    int8_attention_many_kernel<TYPE, D, RT, TOKENS, WGS><<<(unsigned)(p.items * a.kv_heads * p.splits), 64 * kWaves, 0, s>>>(a, (int)p.items);
     return hipGetLastError();
 }
 
@@ -319,8 +319,8 @@ hipError_t launch(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s)
 
 hipError_t launch_attention_many(const AttentionArgs& a, const AttentionPlan& p, int type, int head_dim, hipStream_t s) {
     if (type == WQ_F16)
-        return head_dim == 64 ? launch<WQ_F16, 64, 3, 64>(a, p, s) : head_dim == 128 ? launch<WQ_F16, 128, 3, 32>(a, p, s) : launch<WQ_F16, 256, 1, 32>(a, p, s);
-    return head_dim == 64 ? launch<WQ_BF16, 64, 3, 64>(a, p, s) : head_dim == 128 ? launch<WQ_BF16, 128, 3, 32>(a, p, s) : launch<WQ_BF16, 256, 1, 32>(a, p, s);
+        return head_dim == 64 ? launch<WQ_F16, 64, 2, 64, 3>(a, p, s) : head_dim == 128 ? launch<WQ_F16, 128, 2, 64, 2>(a, p, s) : launch<WQ_F16, 256, 1, 32, 2>(a, p, s);
+    return head_dim == 64 ? launch<WQ_BF16, 64, 2, 64, 3>(a, p, s) : head_dim == 128 ? launch<WQ_BF16, 128, 2, 64, 2>(a, p, s) : launch<WQ_BF16, 256, 1, 32, 2>(a, p, s);
 }
 
 }  // namespace wq

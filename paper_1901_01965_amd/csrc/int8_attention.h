@@ -15,7 +15,8 @@ struct AttentionArgs {
     Batch batch;
     int kv_heads, group;               // heads of queries per head of keys
     int tile_rows, unit, head_tiles;   // a workgroup's rows: up to `unit` of a sequence's, of a group's heads or tile_rows of them
-    int causal, window, splits;
+    int causal, window;
+    int splits, least_steps;           // parts of a sequence at the most, steps of a part at the least
     float scale_log2, sign;            // |scale| / ln 2: exponentials are taken to base 2
 };
 
@@ -53,7 +54,7 @@ __device__ inline void store4(void* out, long long at, v4f v) {
 }
 
 constexpr int kStep = 64;        // tokens a wave or workgroup takes at a time
-constexpr int kLeastSteps = 4;   // of a part of a sequence
+constexpr int kMostParts = 256;  // of a sequence
 
 // A tile's rows and tokens.
 struct Tile {
@@ -80,7 +81,7 @@ __device__ inline bool tile_of(const AttentionArgs& a, int item, int y, Tile& t)
     visible(a, position + t.tokens - 1, t.sequence.length, t.low_all, t.high);
     t.begin = t.low & ~(kStep - 1);
     t.steps = max(ceil_div(t.high - t.begin, kStep), 0);
-    t.per = ceil_div(t.steps, min(a.splits, max(t.steps / kLeastSteps, 1)));
+    t.per = ceil_div(t.steps, min(a.splits, max(t.steps / a.least_steps, 1)));
     return true;
 }
 
@@ -88,7 +89,7 @@ struct AttentionPlan {
     bool many;
     int tile_rows, unit, head_tiles;
     long long items;   // tiles of rows, those of a group's heads aside
-    int splits;
+    int splits, least_steps;
     size_t workspace;
 };
 

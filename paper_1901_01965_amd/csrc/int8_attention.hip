@@ -7,38 +7,43 @@ namespace wq {
 
 namespace {
 
-// Joins the parts of a row: one workgroup per row, its threads share the parts out.
+// Joins the parts of a row, a wave each: its lanes find the parts' factors side by side, then share the parts out.  Bound by the latency
+// of one read of each.
+constexpr int kJoinRows = 4;
+
 template <int TYPE, int D>
-__global__ __launch_bounds__(256) void int8_attention_join_kernel(AttentionArgs a) {
-    constexpr int kAcross = D / 4, kDown = 256 / kAcross;
-    __shared__ v4f sums[kDown][kAcross];
-    __shared__ float totals[kDown];
+__global__ __launch_bounds__(64 * kJoinRows) void int8_attention_join_kernel(AttentionArgs a) {
+    constexpr int kAcross = D / 4, kDown = 64 / kAcross;
+    __shared__ float factors[kJoinRows][kMostParts];
+    const int groups = ceil_div(a.tile_rows, kJoinRows), item = blockIdx.x / groups, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Tile t;
-    if (!tile_of(a, blockIdx.x / a.tile_rows, blockIdx.y, t)) return;
-    const int row = blockIdx.x % a.tile_rows;
+    if (!tile_of(a, item, blockIdx.y, t)) return;
+    const int row = blockIdx.x % groups * kJoinRows + wave;
     if (row >= t.tokens * t.heads || t.per >= t.steps) return;
-    const int parts = ceil_div(t.steps, t.per), across = threadIdx.x % kAcross, down = threadIdx.x / kAcross;
+    const int parts = ceil_div(t.steps, t.per), across = lane % kAcross, down = lane / kAcross;
     const long long each = a.tile_rows * (D + 2);
-    const float* const partial = a.partial + ((long long)(blockIdx.x / a.tile_rows) * gridDim.y + blockIdx.y) * a.splits * each;
-    float all = -INFINITY;
-    for (int p = 0; p < parts; ++p) all = fmaxf(all, partial[p * each + a.tile_rows * D + 2 * row]);
+    const float* const partial = a.partial + ((long long)item * gridDim.y + blockIdx.y) * a.splits * each;
+    const float* const stats = partial + a.tile_rows * D + 2 * row;
+    float all = -INFINITY, total = 0.0f;
+    for (int p = lane; p < parts; p += 64) all = fmaxf(all, stats[p * each]);
+#pragma unroll
+    for (int step = 32; step > 0; step >>= 1) all = fmaxf(all, __shfl_xor(all, step));
+    for (int p = lane; p < parts; p += 64) {
+        const float largest = stats[p * each], factor = largest == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(largest - all);
+        factors[wave][p] = factor;
+        if (largest != -INFINITY) total += stats[p * each + 1] * factor;
+    }
+#pragma unroll
+    for (int step = 32; step > 0; step >>= 1) total += __shfl_xor(total, step);
+    __builtin_amdgcn_wave_barrier();
     v4f r = {};
-    float total = 0.0f;
-    for (int p = down; p < parts; p += kDown) {
-        const float* const part = partial + p * each;
-        const float largest = part[a.tile_rows * D + 2 * row];
-        const float factor = largest == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(largest - all);
-        if (largest != -INFINITY) total += part[a.tile_rows * D + 2 * row + 1] * factor;
-        r += *reinterpret_cast<const v4f*>(part + row * D + 4 * across) * factor;
-    }
-    sums[down][across] = r;
-    if (across == 0) totals[down] = total;
-    __syncthreads();
+#pragma unroll 4
+    for (int p = down; p < parts; p += kDown) r += *reinterpret_cast<const v4f*>(partial + p * each + (long long)row * D + 4 * across) * factors[wave][p];
+#pragma unroll
+    for (int step = kAcross; step < 64; step *= 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] += __shfl_xor(r[i], step);
     if (down != 0) return;
-    for (int i = 1; i < kDown; ++i) {
-        r += sums[i][across];
-        total += totals[i];
-    }
     const float over = total == 0.0f ? 0.0f : 1.0f / total;
     const long long row_at = (long long)(t.sequence.first + t.token0 + row / t.heads);
     store4<TYPE>(a.out, row_at * a.out_stride + (long long)(t.head0 + row % t.heads) * D + 4 * across, r * over);
@@ -46,7 +51,8 @@ __global__ __launch_bounds__(256) void int8_attention_join_kernel(AttentionArgs 
 
 template <int TYPE, int D>
 hipError_t join(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) {
-    int8_attention_join_kernel<TYPE, D><<<dim3((unsigned)(p.items * p.tile_rows), a.kv_heads * a.head_tiles), 256, 0, s>>>(a);
+    const long long groups = p.items * ceil_div(p.tile_rows, kJoinRows);
+    int8_attention_join_kernel<TYPE, D><<<dim3((unsigned)groups, a.kv_heads * a.head_tiles), 64 * kJoinRows, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -68,8 +74,14 @@ AttentionPlan plan_attention(int rows, int heads, int kv_heads, int head_dim, in
         while (has_starts && 2 * p.unit * group <= 16) p.unit *= 2;
     p.items = has_starts ? item_count(rows, sequences, p.unit, 1) : sequences;
     const long long tiles = p.items * kv_heads * p.head_tiles;
-    const long long most = max((long long)width * block / (kStep * kLeastSteps), 1ll);
-    p.splits = (int)min(max(((p.many ? 2ll : 8ll) * kComputeUnits + tiles - 1) / tiles, 1ll), most);
+    // Few tiles: as many parts as give every compute unit a workgroup (two with many rows), of at least one step for each wave.  Enough
+    // tiles: four parts each, of at least two steps for each wave, so that what is left of the longest sequences at the end is small
+    // (64 sequences, 8 heads of keys, 500 to 8192 tokens: 140 us unsplit, 127 so; one of 30000 among 1500: 358 and 126; all of 4096: 102
+    // and 113).
+    const bool enough = !p.many && tiles >= kComputeUnits;
+    p.least_steps = enough ? 8 : 4;
+    const long long most = min(max((long long)width * block / (kStep * p.least_steps), 1ll), (long long)kMostParts);
+    p.splits = (int)min(enough ? 4ll : ((p.many ? 2ll : 1ll) * kComputeUnits + tiles - 1) / tiles, most);
     p.workspace = p.splits > 1 ? (size_t)tiles * p.splits * p.tile_rows * (head_dim + 2) * sizeof(float) : 0;
     return p;
 }
@@ -114,7 +126,7 @@ int int8_cache_attention(const void* q_dev, long long q_stride, int type, int ro
     const AttentionArgs a = {q_dev, q_stride, out_dev, out_stride, cache_k_dev, cache_v_dev, k_scale_dev, v_scale_dev,
                              static_cast<float*>(workspace_dev),
                              {table_dev, lengths_dev, starts_dev, table_width, sequences, rows, blocks, block_shift(block)},
-                             kv_heads, heads / kv_heads, p.tile_rows, p.unit, p.head_tiles, causal != 0, window, p.splits,
+                             kv_heads, heads / kv_heads, p.tile_rows, p.unit, p.head_tiles, causal != 0, window, p.splits, p.least_steps,
                              fabsf(scale) * 1.44269504088896340736f, scale < 0.0f ? -1.0f : 1.0f};
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
     if (hipError_t e = (p.many ? launch_attention_many : launch_attention_rows)(a, p, type, head_dim, s)) return status_of(e);

@@ -59,7 +59,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int4_tiles_kernel(const typena
     constexpr int kGroups = kTileInputs / GROUP, kSteps = GROUP / 32;
     constexpr int kPieces = kTileInputs * sizeof(T) / 16;          // 16-byte pieces of a row of the tile
     constexpr int kLoads = kRows * kPieces / (64 * kWaves);        // a thread's
-    __shared__ v4u held[2][kRows * kPieces];
+    // two arrays, each known by name wherever it is read or written: of one, reads would wait for what is on its way into the other half
+    __shared__ v4u even[kRows * kPieces], odd[kRows * kPieces];
+    typedef v4u Held[kRows * kPieces];
     __shared__ v4u codes[kWaves][NT][64];                          // each wave's own
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, quarter = lane >> 4;
@@ -83,24 +85,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int4_tiles_kernel(const typena
     // thread -> (row, piece) of the tile as it lies in LDS: from load to load the same distance for all
     const int my_row = threadIdx.x / kPieces, my_piece = (threadIdx.x % kPieces) ^ (my_row & (kPieces - 1));
     const uint32_t my_bytes = (uint32_t)(my_row * x_stride * sizeof(T)) + 16 * my_piece;
-    auto fetch = [&](int kt, int half) {
+    auto fetch = [&](int kt, Held& held) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const char* const from = reinterpret_cast<const char*>(x + (long long)(m0 + i * 64 * kWaves / kPieces) * x_stride + kt * kTileInputs);
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + my_bytes),
-                                             (__attribute__((address_space(3))) void*)(&held[half][i * 64 * kWaves + wave * 64]), 16, 0, 0);
+                                             (__attribute__((address_space(3))) void*)(&held[i * 64 * kWaves + wave * 64]), 16, 0, 0);
         }
     };
     // eight inputs of row 16 mt + row, from 32 step + 8 quarter on
-    auto inputs = [&](int half, int mt, int step) {
+    auto inputs = [&](const Held& held, int mt, int step) {
         const int r = 16 * mt + row;
         if constexpr (XT == WQ_I8) {
             const int piece = 2 * step + (quarter >> 1);
-            const v2u* const p = reinterpret_cast<const v2u*>(&held[half][r * kPieces + (piece ^ (r & (kPieces - 1)))]) + (quarter & 1);
+            const v2u* const p = reinterpret_cast<const v2u*>(&held[r * kPieces + (piece ^ (r & (kPieces - 1)))]) + (quarter & 1);
             return __builtin_bit_cast(long, *p);
         } else {
             const int piece = 4 * step + quarter;
-            return P::activations(held[half][r * kPieces + (piece ^ (r & (kPieces - 1)))]);
+            return P::activations(held[r * kPieces + (piece ^ (r & (kPieces - 1)))]);
         }
     };
 
@@ -123,13 +125,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int4_tiles_kernel(const typena
     v4f acc[NT][kRowTiles] = {};
     Factors next;
     fetch_codes(0);
-    fetch(0, 0);
+    fetch(0, even);
     fetch_factors(next, 0);
-    for (int kt = 0; kt < w.input_tiles; ++kt) {
-        const int half = kt & 1;
+    auto multiply = [&](int kt, const Held& held, Held& other) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's share of the tile is there
         __syncthreads();                                   // everyone's is, and the other half has been read
-        if (kt + 1 < w.input_tiles) fetch(kt + 1, half ^ 1);
+        if (kt + 1 < w.input_tiles) fetch(kt + 1, other);
 #pragma unroll 1
         for (int group = 0; group < kGroups; ++group) {
             typename P::Fragment ws[NT][kSteps];
@@ -149,7 +150,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int4_tiles_kernel(const typena
             fetch_factors(next, kt * kGroups + group + 1);
             typename P::Fragment xs[2][kSteps];
 #pragma unroll
-            for (int j = 0; j < kSteps; ++j) xs[0][j] = inputs(half, 0, group * kSteps + j);
+            for (int j = 0; j < kSteps; ++j) xs[0][j] = inputs(held, 0, group * kSteps + j);
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);
             // the products of 16 rows, and between them the multiply-adds of the 16 before
@@ -158,7 +159,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int4_tiles_kernel(const typena
             for (int mt = 0; mt <= kRowTiles; ++mt) {
                 if (mt + 1 < kRowTiles)
 #pragma unroll
-                    for (int j = 0; j < kSteps; ++j) xs[(mt + 1) & 1][j] = inputs(half, mt + 1, group * kSteps + j);
+                    for (int j = 0; j < kSteps; ++j) xs[(mt + 1) & 1][j] = inputs(held, mt + 1, group * kSteps + j);
                 if (mt < kRowTiles) {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) sums[mt & 1][nt] = typename P::Sum{};
@@ -184,6 +185,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int4_tiles_kernel(const typena
             }
             __builtin_amdgcn_s_setprio(0);
         }
+    };
+    for (int kt = 0; kt < w.input_tiles; kt += 2) {
+        multiply(kt, even, odd);
+        if (kt + 1 < w.input_tiles) multiply(kt + 1, odd, even);
     }
     if (!fits) return;
 #pragma unroll
@@ -211,11 +216,12 @@ inline long long rounds(const Int4Weights& w, const Int4Output& o, int nt) {
 template <int XT>
 hipError_t launch_tiles_of(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
     return with_weights(w, [&](auto group, auto zeros, auto bf16) {
-        // Three tiles of outputs a wave ask a third less of the LDS per product than two, which bounds float16 (8192 rows through
-        // 4096 x 28672: 1710 against 1850 us; int8 asks half as much: 210 against 190 us for 4096 rows through 4096 x 8192), where their
-        // coarser rounds do not cost more (2048 rows through 4096 x 4096: 80 against 67 us).
-        if constexpr (XT == WQ_F16)
-            if (rounds(w, o, 3) * 1.5 * 0.92 < rounds(w, o, 2)) return launch<XT, group(), zeros(), bf16(), 3>(x, x_stride, w, o, s);
+        // More tiles of outputs a wave read LDS less often per product, in coarser rounds.  Measured against two, alike in rounds: three
+        // 0.82 (float16 in groups of 128, whose operands leave no room for four: 4096 rows through 4096 x 8192 260 against 280 us, 8192
+        // through 4096 x 28672 1660 and 1797; but 2048 through 4096 x 4096 80 and 70), four 0.92 (int8 183 and 197, groups of 64 264 and 295).
+        constexpr int kMore = XT == WQ_F16 && group() == 128 ? 3 : 4;
+        constexpr double kCost = kMore == 3 ? 0.82 * 1.5 : 0.92 * 2;
+        if (rounds(w, o, kMore) * kCost < rounds(w, o, 2)) return launch<XT, group(), zeros(), bf16(), kMore>(x, x_stride, w, o, s);
         return launch<XT, group(), zeros(), bf16(), 2>(x, x_stride, w, o, s);
     });
 }

@@ -65,6 +65,15 @@ def test_every_size_against_64_bits(M, N, K, group, zeros, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16, I8])
+@pytest.mark.parametrize("group,zeros", [(32, False), (64, True), (128, False), (128, True)])
+def test_enough_rows_and_outputs_for_coarser_tiles(group, zeros, dtype):
+    M, N, K = 1101, 8200, 384
+    x, codes, scales, zero = make(M, N, K, group, dtype, zeros, seed=2)
+    got = wg.int4_linear(x, wg.pack_int4_weights(codes, scales, zero, group))
+    check(got, *reference(x, codes, scales, zero, group), dtype, K, group)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, I8])
 @pytest.mark.parametrize("out_dtype", [F16, BF16, F32])
 @pytest.mark.parametrize("M", [3, 40, 200])
 def test_bias_relu_scales_of_rows_and_types_of_the_result(M, out_dtype, dtype):

@@ -33,9 +33,10 @@ size_t int4_packed_bytes(int N, int K, int group, int has_zeros);
 int int4_pack_weights(const uint8_t* codes_dev, const void* scales_dev, int scale_type, const uint8_t* zeros_dev, int N, int K,
                       int group, void* packed_dev, size_t packed_bytes, void* hip_stream);
 
-/* Scratch bytes int4_linear needs for such a call; 0 if it needs none or the arguments are invalid.  (Many rows are read in tiles: of
- * rows that are not, a copy is made; bfloat16 rows become float16, times a power of two each.) */
-size_t int4_linear_workspace_bytes(const void* x_dev, int x_type, long long x_stride, int M, int K);
+/* Scratch bytes int4_linear needs for such a call; 0 if it needs none or the arguments are invalid.  (Rows are
+ * read in 16-byte pieces, many of them in tiles: of rows that do not consist of such, a copy is made; many bfloat16 rows become
+ * float16, times a power of two each.) */
+size_t int4_linear_workspace_bytes(const void* x_dev, int x_type, long long x_stride, int M, int N, int K);
 
 /* x: [M][K] of x_type WQ_F16, WQ_BF16 or WQ_I8, rows x_stride elements apart (x_stride >= K).  x_scale: float [M], only for
  * WQ_I8, or NULL.  bias: float [N] or NULL.  y: dense [M][N] of y_type WQ_F16, WQ_BF16 or WQ_F32.  The blob has to be the one

@@ -9,9 +9,9 @@ bool valid_weights(int N, int K, int group) {
     return N > 0 && K > 0 && (group == 32 || group == 64 || group == 128);
 }
 
-// Keeps every count an int and every launch below 2^32 threads: 2^34 codes, 2^26 outputs.
+// Keeps every count an int and every launch below 2^32 threads: 2^34 codes, 2^22 outputs.
 bool too_large(int N, int K) {
-    return N > (1 << 26) || K > (1 << 26) || (long long)ceil_div(N, kTileOutputs) * ceil_div(K, kTileInputs) > (1 << 23);
+    return N > (1 << 22) || K > (1 << 26) || (long long)ceil_div(N, kTileOutputs) * ceil_div(K, kTileInputs) > (1 << 23);
 }
 
 Int4Weights weights_of(const void* blob, int N, int K, int group, int scale_type, int has_zeros) {
@@ -50,10 +50,10 @@ __global__ void int4_pack_kernel(const uint8_t* codes, const uint16_t* scales, c
     }
 }
 
-// Rows as the kernel for many rows reads them: whole tiles of inputs with zeros behind the last, 16-byte aligned.  bfloat16 becomes
+// Rows as the kernels read them: whole tiles of inputs with zeros behind the last, 16-byte aligned.  HALF, for many rows: bfloat16 becomes
 // float16, brought by a power of two per row to a largest magnitude of 2^14 .. 2^15: its eight bits fit, down to 2^-28 of that, and
 // `factors` takes the power off again.  One workgroup per row, bound by the bytes.
-template <int XT>
+template <int XT, bool HALF>
 __global__ __launch_bounds__(256) void int4_rows_in_order_kernel(const typename Element<XT>::type* x, long long x_stride, typename Element<XT>::type* out,
                                                                  float* factors, int K, int padded) {
     typedef typename Element<XT>::type T;
@@ -62,10 +62,10 @@ __global__ __launch_bounds__(256) void int4_rows_in_order_kernel(const typename 
     const T* const row = x + (long long)blockIdx.x * x_stride;
     T* const to = out + (long long)blockIdx.x * padded;
     float up = 1.0f;
-    if constexpr (XT == WQ_BF16) {
+    if constexpr (HALF) {
         float most = 0.0f;
         for (int k = 8 * threadIdx.x; k < K; k += 8 * 256) {
-            const V v = __builtin_bit_cast(V, load_inputs<XT>(row, k, K, false));
+            const V v = __builtin_bit_cast(V, load_inputs<XT>(row, k, K));
 #pragma unroll
             for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf((float)v[j]));
         }
@@ -79,8 +79,8 @@ __global__ __launch_bounds__(256) void int4_rows_in_order_kernel(const typename 
         if (threadIdx.x == 0) factors[blockIdx.x] = down;
     }
     for (int k = 8 * threadIdx.x; k < padded; k += 8 * 256) {
-        const V v = __builtin_bit_cast(V, load_inputs<XT>(row, k, K, false));
-        if constexpr (XT == WQ_BF16) {
+        const V v = __builtin_bit_cast(V, load_inputs<XT>(row, k, K));
+        if constexpr (HALF) {
             v8h h;
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[j] = (_Float16)((float)v[j] * up);
@@ -91,14 +91,15 @@ __global__ __launch_bounds__(256) void int4_rows_in_order_kernel(const typename 
     }
 }
 
-hipError_t launch_rows_in_order(const void* x, int x_type, long long x_stride, void* out, float* factors, int M, int K, int padded, hipStream_t s) {
-    if (x_type == WQ_BF16)
-        int4_rows_in_order_kernel<WQ_BF16><<<M, 256, 0, s>>>(static_cast<const __bf16*>(x), x_stride, static_cast<__bf16*>(out), factors, K, padded);
-    else if (x_type == WQ_F16)
-        int4_rows_in_order_kernel<WQ_F16><<<M, 256, 0, s>>>(static_cast<const _Float16*>(x), x_stride, static_cast<_Float16*>(out), factors, K, padded);
-    else
-        int4_rows_in_order_kernel<WQ_I8><<<M, 256, 0, s>>>(static_cast<const int8_t*>(x), x_stride, static_cast<int8_t*>(out), factors, K, padded);
-    return hipGetLastError();
+hipError_t launch_rows_in_order(const void* x, int x_type, bool half, long long x_stride, void* out, float* factors, int M, int K, int padded, hipStream_t s) {
+    const auto run = [&](auto type, auto as_half) {
+        typedef typename Element<type()>::type T;
+        int4_rows_in_order_kernel<type(), as_half()><<<M, 256, 0, s>>>(static_cast<const T*>(x), x_stride, static_cast<T*>(out), factors, K, padded);
+        return hipGetLastError();
+    };
+    if (x_type == WQ_I8) return run(std::integral_constant<int, WQ_I8>(), std::false_type());
+    // without a change of type 16 bits are 16 bits
+    return half ? run(std::integral_constant<int, WQ_BF16>(), std::true_type()) : run(std::integral_constant<int, WQ_F16>(), std::false_type());
 }
 
 // Which kernel a call runs, and what it needs of a workspace: a copy of the rows, and one factor each.
@@ -107,14 +108,19 @@ struct Int4Plan {
     int padded;
     size_t factors, total;   // bytes
 };
-Int4Plan plan_int4(const void* x, int x_type, long long x_stride, int M, int K) {
-    Int4Plan p = {M > 64, false, ceil_div(K, kTileInputs) * kTileInputs, 0, 0};
+// The kernel for many rows takes about 1.2 us per tile of inputs however few workgroups it has, the one for few rows 2.7e-5 us per 4096
+// inputs of every element of y (float16, 4096 inputs: 38 and 30 us for 256 rows and 4096 outputs, 38 and 43 for 384; 40 and 31 us for 64 rows
+// and 16384 outputs, 41 and 44 for 96).
+constexpr long long kManyElements = 1400000;
+
+Int4Plan plan_int4(const void* x, int x_type, long long x_stride, int M, int N, int K) {
+    Int4Plan p = {M > 32 && (long long)M * N > kManyElements, false, ceil_div(K, kTileInputs) * kTileInputs, 0, 0};
     const size_t size = x_type == WQ_I8 ? 1 : 2;
-    if (!p.many) return p;
-    p.copy = x_type == WQ_BF16 || M < kTileRows || K % kTileInputs != 0 || (x_stride * size) % 16 != 0 || !aligned(x, 16) || x_stride > (1 << 24);
+    // both kernels read whole aligned pieces of rows, the one for many rows also whole tiles only
+    p.copy = (x_stride * size) % 16 != 0 || !aligned(x, 16) || x_stride > (1 << 24) || (p.many && (x_type == WQ_BF16 || M < kTileRows || K % kTileInputs != 0));
     if (!p.copy) return p;
-    p.factors = (((size_t)max(M, kTileRows) * p.padded * size) + 255) & ~(size_t)255;
-    p.total = p.factors + (x_type == WQ_BF16 ? (size_t)M * sizeof(float) : 0);
+    p.factors = (((size_t)(p.many ? max(M, kTileRows) : M) * p.padded * size) + 255) & ~(size_t)255;
+    p.total = p.factors + (p.many && x_type == WQ_BF16 ? (size_t)M * sizeof(float) : 0);
     return p;
 }
 
@@ -147,9 +153,9 @@ int int4_pack_weights(const uint8_t* codes_dev, const void* scales_dev, int scal
     return status_of(launch_int4_pack(codes_dev, scales_dev, zeros_dev, w, static_cast<uint8_t*>(packed_dev), static_cast<hipStream_t>(hip_stream)));
 }
 
-size_t int4_linear_workspace_bytes(const void* x_dev, int x_type, long long x_stride, int M, int K) {
-    if (!(is_half(x_type) || x_type == WQ_I8) || M <= 0 || K <= 0 || K > (1 << 26)) return 0;
-    return plan_int4(x_dev, x_type, x_stride, M, K).total;
+size_t int4_linear_workspace_bytes(const void* x_dev, int x_type, long long x_stride, int M, int N, int K) {
+    if (!(is_half(x_type) || x_type == WQ_I8) || M <= 0 || N <= 0 || K <= 0 || too_large(N, K)) return 0;
+    return plan_int4(x_dev, x_type, x_stride, M, N, K).total;
 }
 
 int int4_linear(const void* x_dev, int x_type, long long x_stride, const float* x_scale_dev, const void* packed_dev,
@@ -163,8 +169,8 @@ int int4_linear(const void* x_dev, int x_type, long long x_stride, const float* 
     if (!x_dev || !y_dev) return WG_EINVAL;
     if (!aligned(packed_dev, 256) || !aligned(y_dev, y_type == WQ_F32 ? 4 : 2) || !aligned(x_dev, x_type == WQ_I8 ? 1 : 2)) return WG_EINVAL;
     if (!aligned(x_scale_dev, 4) || !aligned(bias_dev, 4)) return WG_EINVAL;
-    if (too_large(N, K) || M > (1 << 23)) return WG_EUNSUPPORTED;
-    const Int4Plan p = plan_int4(x_dev, x_type, x_stride, M, K);
+    if (too_large(N, K) || M > (1 << 23) || (long long)M * N > 1ll << 36) return WG_EUNSUPPORTED;
+    const Int4Plan p = plan_int4(x_dev, x_type, x_stride, M, N, K);
     if (p.total > 0) {
         if (!workspace_dev || !aligned(workspace_dev, 256)) return WG_EINVAL;
         if (workspace_bytes < p.total) return WG_ESMALLBUF;
@@ -174,10 +180,10 @@ int int4_linear(const void* x_dev, int x_type, long long x_stride, const float* 
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
     if (p.copy) {
         float* const factors = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + p.factors);
-        if (hipError_t e = launch_rows_in_order(x_dev, x_type, x_stride, workspace_dev, factors, M, K, p.padded, s)) return status_of(e);
+        if (hipError_t e = launch_rows_in_order(x_dev, x_type, p.many && x_type == WQ_BF16, x_stride, workspace_dev, factors, M, K, p.padded, s)) return status_of(e);
         x_dev = workspace_dev;
         x_stride = p.padded;
-        if (x_type == WQ_BF16) o.x_scale = factors;
+        if (p.many && x_type == WQ_BF16) o.x_scale = factors;
     }
     const auto launch = p.many ? (x_type == WQ_I8 ? launch_int4_tiles_int8 : launch_int4_tiles_half)
                       : x_type == WQ_F16 ? launch_int4_rows_half : x_type == WQ_BF16 ? launch_int4_rows_bfloat : launch_int4_rows_int8;

@@ -1,10 +1,14 @@
 // y = x W^T with 4-bit weights for few rows: the weights' bytes are read once, everything else stays beside them.
 //
-// A workgroup takes 16 NT outputs and 16 MT rows; its waves share the inputs out by tiles of 128 and add their sums up in LDS at the
-// end, in the order of the waves.  The matrix cores multiply (rows beyond the last are copies of it and are not stored): a word of
+// A workgroup takes 16 NT outputs and up to ROWS rows; its up to WAVES waves share the inputs out by tiles of 128 and add their sums up in LDS at the
+// end, in the order of the waves.  The matrix cores multiply (rows beyond the last are copies of others and are not stored): a word of
 // eight codes costs seven vector instructions as float16 and three as int8 (int4_weights.h), the sum over a group of sum_k x_k that
 // takes the zero points off is one more product, whose other operand is constant, and becomes the accumulator that the codes'
 // products start from.
+//
+// Every workgroup reads all activations, which for 16 rows are more bytes than its weights: they come into the wave's own part of the
+// LDS in whole lines and without registers, a tile ahead like the codes (as operands, 64 bytes of a row at a time, they held the kernel
+// at 21.6 us for 16 rows through 8192 x 8192, against 11.8 with their reads all of one tile).
 #pragma once
 #include "int4_weights.h"
 
@@ -12,78 +16,118 @@ namespace wq {
 
 namespace {
 
-constexpr int kMostWaves = 8;
-
-template <int XT, int GROUP, bool ZEROS, bool BF16, int MT, int NT, int AHEAD>
-__global__ __launch_bounds__(64 * kMostWaves) void int4_rows_kernel(const typename Element<XT>::type* x, long long x_stride, Int4Weights w, Int4Output o) {
+template <int XT, int GROUP, bool ZEROS, bool BF16, int ROWS, int NT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void int4_rows_kernel(const typename Element<XT>::type* x, long long x_stride, Int4Weights w, Int4Output o,
+                                                               int row_blocks) {
+    typedef typename Element<XT>::type T;
     typedef Products<XT> P;
-    typedef std::conditional_t<XT == WQ_I8, v2u, v4u> Bits;
+    constexpr int MT = (ROWS + 15) / 16;
     constexpr int kGroups = kTileInputs / GROUP, kSteps = GROUP / 32;   // groups in a tile, products in a group
-    __shared__ v4f sums[kMostWaves][NT * MT][64];
+    constexpr int kPieces = kTileInputs * sizeof(T) / 16;               // 16-byte pieces of a row of a tile
+    constexpr int kHeld = ROWS * kPieces < 64 ? 64 / kPieces : ROWS;    // rows that a tile of activations holds
+    constexpr int kLoads = kHeld * kPieces / 64;                        // of 16 bytes a lane
+    // a wave's tile, row by row, piece c of row r at c ^ r (a row's pieces apart); two arrays, each known by name wherever it is used: of
+    // one, reads would wait for what is on its way into the other half
+    typedef v4u Held[kHeld * kPieces];
+    __shared__ Held even[WAVES], odd[WAVES];
+    __shared__ v4f sums[WAVES][NT * MT][64];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    const int tile0 = blockIdx.x * NT, m0 = blockIdx.y * (16 * MT);
+    const int row = lane & 15, quarter = lane >> 4;
+    // blocks of rows that read the same weights follow each other on an XCD
+    const int turn = blockIdx.x >> 3, tile0 = (turn / row_blocks * 8 + (blockIdx.x & 7)) * NT, m0 = turn % row_blocks * ROWS;
+    if (tile0 >= w.output_tiles) return;
     const bool fits = matches(w);
+    const uint32_t one = in_lanes(P::kOne);
 
-    const typename Element<XT>::type* row[MT];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) row[mt] = x + (long long)min(m0 + 16 * mt + (lane & 15), o.M - 1) * x_stride;
-    const v4u* codes[NT];
-    size_t scale_at[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const size_t tile = min(tile0 + nt, w.output_tiles - 1);
-        codes[nt] = reinterpret_cast<const v4u*>(w.codes + tile * w.input_tiles * kTileBytes) + lane;
-        scale_at[nt] = tile * w.groups * kTileOutputs + 4 * (lane >> 4);
-    }
-
-    // what a tile of inputs needs, on its way while earlier ones are multiplied
+    // what a tile of inputs needs beside its activations
     struct Stage {
         v4u words[NT];
         v2u scales[NT][kGroups];
         uint32_t zeros[NT][kGroups];
-        Bits x[4][MT];
     };
-    auto load = [&](Stage& t, int kt, bool whole) {
+    auto load_codes = [&](Stage& t, int kt) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            t.words[nt] = codes[nt][(size_t)kt * (kTileBytes / 16)];
+            const size_t tile = min(tile0 + nt, w.output_tiles - 1);
+            t.words[nt] = reinterpret_cast<const v4u*>(w.codes + (tile * w.input_tiles + kt) * kTileBytes)[lane];
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
-                const size_t at = scale_at[nt] + (size_t)(kt * kGroups + g) * kTileOutputs;
+                const size_t at = (tile * w.groups + (size_t)kt * kGroups + g) * kTileOutputs + 4 * quarter;
                 t.scales[nt][g] = *reinterpret_cast<const v2u*>(w.scales + at);
                 t.zeros[nt][g] = ZEROS ? *reinterpret_cast<const uint32_t*>(w.zeros + at) : 0;
             }
         }
+    };
+    auto place = [&](int i, int& r, int& piece) {
+        r = i * (64 / kPieces) + lane / kPieces;
+        piece = (lane % kPieces) ^ (r & (kPieces - 1));
+    };
+    const T* from[kLoads];
 #pragma unroll
-        for (int step = 0; step < 4; ++step)
+    for (int i = 0; i < kLoads; ++i) {
+        int r, piece;
+        place(i, r, piece);
+        from[i] = x + (long long)min(m0 + r, o.M - 1) * x_stride + piece * (16 / (int)sizeof(T));
+    }
+    auto bring = [&](Held& held, int kt) {
+        // what lay there has been read (the compiler knows of no one but the transfers that writes there, and takes its own reads past any
+        // wait; past a fence it does not)
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-                t.x[step][mt] = load_inputs<XT>(row[mt], kt * kTileInputs + 32 * step + 8 * (lane >> 4), w.K, whole);
+        for (int i = 0; i < kLoads; ++i)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from[i] + kt * kTileInputs),
+                                             (__attribute__((address_space(3))) void*)(&held[64 * i]), 16, 0, 0);
+    };
+    // the last tile, where inputs end inside it
+    auto bring_rest = [&](Held& held, int kt) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            int r, piece;
+            place(i, r, piece);
+            const T* const begin = x + (long long)min(m0 + r, o.M - 1) * x_stride;
+            const int k = kt * kTileInputs + piece * (16 / (int)sizeof(T));
+            if constexpr (XT == WQ_I8) {
+                const v2u a = load_inputs<XT>(begin, k, w.K), b = load_inputs<XT>(begin, k + 8, w.K);
+                held[64 * i + lane] = v4u{a[0], a[1], b[0], b[1]};
+            } else {
+                held[64 * i + lane] = load_inputs<XT>(begin, k, w.K);
+            }
+        }
+    };
+    // eight inputs of row 16 mt + row, from 32 step + 8 quarter on
+    auto inputs = [&](const Held& held, int mt, int step) {
+        const int r = (16 * mt + row) % kHeld;
+        if constexpr (XT == WQ_I8) {
+            const int piece = 2 * step + (quarter >> 1);
+            return P::activations(reinterpret_cast<const v2u*>(&held[r * kPieces + (piece ^ (r & (kPieces - 1)))])[quarter & 1]);
+        } else {
+            return P::activations(held[r * kPieces + ((4 * step + quarter) ^ (r & (kPieces - 1)))]);
+        }
     };
 
     v4f acc[NT][MT] = {};
     const typename P::Fragment ones = P::ones(ZEROS);
-    auto multiply = [&](const Stage& t) {
-        typename P::Fragment xs[4][MT];
-#pragma unroll
-        for (int step = 0; step < 4; ++step)
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) xs[step][mt] = P::activations(t.x[step][mt]);
+    auto multiply = [&](const Stage& t, const Held& held) {
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
+            typename P::Fragment xs[kSteps][MT];
             typename P::Sum off[MT];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 off[mt] = typename P::Sum{};
 #pragma unroll
-                for (int j = 0; j < kSteps; ++j) off[mt] = P::multiply(ones, xs[g * kSteps + j][mt], off[mt]);
+                for (int j = 0; j < kSteps; ++j) {
+                    xs[j][mt] = inputs(held, mt, g * kSteps + j);
+                    off[mt] = P::multiply(ones, xs[j][mt], off[mt]);
+                }
             }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 typename P::Fragment ws[kSteps];
 #pragma unroll
-                for (int j = 0; j < kSteps; ++j) ws[j] = P::weights(t.words[nt][g * kSteps + j]);
+                for (int j = 0; j < kSteps; ++j) ws[j] = P::weights(t.words[nt][g * kSteps + j], one);
                 const v4f scale = scales_of<BF16>(t.scales[nt][g]);
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
@@ -92,7 +136,7 @@ __global__ __launch_bounds__(64 * kMostWaves) void int4_rows_kernel(const typena
 #pragma unroll
                         for (int i = 0; i < 4; ++i) sum[i] = P::times_zero(off[mt][i], (int)(t.zeros[nt][g] >> (8 * i) & 255));
 #pragma unroll
-                    for (int j = 0; j < kSteps; ++j) sum = P::multiply(ws[j], xs[g * kSteps + j][mt], sum);
+                    for (int j = 0; j < kSteps; ++j) sum = P::multiply(ws[j], xs[j][mt], sum);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) acc[nt][mt][i] = __builtin_fmaf((float)sum[i], scale[i], acc[nt][mt][i]);
                 }
@@ -101,23 +145,45 @@ __global__ __launch_bounds__(64 * kMostWaves) void int4_rows_kernel(const typena
     };
 
     const int whole_tiles = w.K / kTileInputs, count = max(whole_tiles - wave + waves - 1, 0) / waves;
-    Stage ahead[AHEAD];
-    auto tile = [&](int i) { return wave + min(i, count - 1) * waves; };
+    Held &mine = even[wave], &other = odd[wave];
+    Stage now, next;
+    // At a wait at least the kLoads transfers of the tile after are younger than the tile's own: with no more than that many requests in
+    // flight it is there, whatever else has been asked for in between.
+    auto arrived = [](auto younger) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(younger()) : "memory");
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    };
+    const std::integral_constant<int, kLoads> but_the_next;
+    const std::integral_constant<int, 0> all;
+    auto tile = [&](int i) { return wave + i * waves; };
     if (count > 0) {
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) load(ahead[u], tile(u), true);
-        for (int i = 0; i < count; i += AHEAD) {
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                if (i + u >= count) break;
-                multiply(ahead[u]);
-                load(ahead[u], tile(i + u + AHEAD), true);
+        bring(mine, tile(0));
+        load_codes(now, tile(0));
+        for (int i = 0;; i += 2) {
+            if (i + 1 == count) {
+                arrived(all);
+                multiply(now, mine);
+                break;
             }
+            bring(other, tile(i + 1));
+            arrived(but_the_next);
+            load_codes(next, tile(i + 1));
+            multiply(now, mine);
+            if (i + 2 == count) {
+                arrived(all);
+                multiply(next, other);
+                break;
+            }
+            bring(mine, tile(i + 2));
+            arrived(but_the_next);
+            load_codes(now, tile(i + 2));
+            multiply(next, other);
         }
     }
     if (whole_tiles < w.input_tiles && wave == whole_tiles % waves) {
-        load(ahead[0], whole_tiles, false);
-        multiply(ahead[0]);
+        bring_rest(mine, whole_tiles);
+        load_codes(now, whole_tiles);
+        multiply(now, mine);
     }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -126,30 +192,43 @@ __global__ __launch_bounds__(64 * kMostWaves) void int4_rows_kernel(const typena
     __syncthreads();
     if (!fits) return;
     for (int e = threadIdx.x; e < NT * MT * 64; e += blockDim.x) {
-        const int tile = e >> 6, l = e & 63;
+        const int tile = e >> 6, l = e & 63, r = 16 * (tile % MT) + (l & 15);
+        if (r >= ROWS) continue;
         v4f total = sums[0][tile][l];
         for (int v = 1; v < waves; ++v) total += sums[v][tile][l];
-        store_outputs(o, m0 + 16 * (tile % MT) + (l & 15), (tile0 + tile / MT) * kTileOutputs + 4 * (l >> 4), total, P::kUnit);
+        store_outputs(o, m0 + r, (tile0 + tile / MT) * kTileOutputs + 4 * (l >> 4), total, P::kUnit);
     }
 }
 
-template <int XT, int GROUP, bool ZEROS, bool BF16, int MT, int NT>
+template <int XT, int GROUP, bool ZEROS, bool BF16, int ROWS, int NT, int WAVES>
 hipError_t launch(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
-    const dim3 grid(ceil_div(w.output_tiles, NT), ceil_div(o.M, 16 * MT));
-    if (grid.y > 65535) return hipErrorInvalidValue;
-    const int waves = min(kMostWaves, w.input_tiles);
-    constexpr int kAhead = MT * (XT == WQ_I8 ? 1 : 2) + NT <= 4 ? 4 : MT <= 2 ? 3 : 2;
-    int4_rows_kernel<XT, GROUP, ZEROS, BF16, MT, NT, kAhead><<<grid, 64 * waves, 0, s>>>(static_cast<const typename Element<XT>::type*>(x), x_stride, w, o);
+    const int row_blocks = ceil_div(o.M, ROWS);
+    const long long blocks = (long long)ceil_div(ceil_div(w.output_tiles, NT), 8) * 8 * row_blocks;
+    int4_rows_kernel<XT, GROUP, ZEROS, BF16, ROWS, NT, WAVES><<<(unsigned)blocks, 64 * min(WAVES, w.input_tiles), 0, s>>>(
+        static_cast<const typename Element<XT>::type*>(x), x_stride, w, o, row_blocks);
     return hipGetLastError();
 }
 
+// How many tiles of outputs a workgroup takes and how many waves: what keeps about 16 waves on every compute unit, with the activations
+// read by as few workgroups as that allows.  (Cold weights; 16 rows: 4096 outputs of 25088 int8 inputs 16.6 us with one tile and 16 waves, 22.3
+// with eight; 8192 of 8192 13.3 with two tiles, 16.6 with one; 16384 of 4096 10.7 with four, 12.8 with two.  One row: 28672 of 4096 14.9
+// with four waves, 16.6 with eight.  32 rows: 8192 of 8192 15.7 with two tiles, 23.5 with one.)
 template <int XT>
 hipError_t launch_rows_of(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
     return with_weights(w, [&](auto group, auto zeros, auto bf16) {
-        const bool pairs = w.output_tiles >= 2 * kComputeUnits;
-        if (o.M <= 16) return (pairs ? launch<XT, group(), zeros(), bf16(), 1, 2> : launch<XT, group(), zeros(), bf16(), 1, 1>)(x, x_stride, w, o, s);
-        if (o.M <= 32) return (pairs ? launch<XT, group(), zeros(), bf16(), 2, 2> : launch<XT, group(), zeros(), bf16(), 2, 1>)(x, x_stride, w, o, s);
-        return (pairs ? launch<XT, group(), zeros(), bf16(), 4, 2> : launch<XT, group(), zeros(), bf16(), 4, 1>)(x, x_stride, w, o, s);
+        const auto run = [&](auto rows, auto tiles, auto waves) { return launch<XT, group(), zeros(), bf16(), rows(), tiles(), waves()>(x, x_stride, w, o, s); };
+        const std::integral_constant<int, 1> one;
+        const std::integral_constant<int, 2> two;
+        const std::integral_constant<int, 4> four;
+        const std::integral_constant<int, 8> eight;
+        const std::integral_constant<int, 16> sixteen;
+        const std::integral_constant<int, 32> thirty_two;
+        const int tiles = w.output_tiles;
+        if (o.M <= 4) return tiles <= kComputeUnits ? run(four, one, sixteen) : tiles < 2 * kComputeUnits ? run(four, one, eight)
+                           : tiles <= 4 * kComputeUnits ? run(four, two, eight) : run(four, two, four);
+        if (o.M <= 16) return tiles <= kComputeUnits ? run(sixteen, one, sixteen) : tiles < 2 * kComputeUnits ? run(sixteen, one, eight)
+                            : tiles < 4 * kComputeUnits ? run(sixteen, two, eight) : run(sixteen, four, eight);
+        return tiles < kComputeUnits ? run(thirty_two, one, eight) : run(thirty_two, two, eight);
     });
 }
 

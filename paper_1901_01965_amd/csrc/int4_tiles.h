@@ -31,8 +31,8 @@ template <> struct Exact<WQ_F16> {
         const uint32_t h = __builtin_bit_cast(uint16_t, (_Float16)(-(16 + z) * 0.0625f));
         return h | h << 16;
     }
-    __device__ static v8h weights(uint32_t w, uint32_t zero) {
-        const v8h v = Products<WQ_F16>::weights(w);
+    __device__ static v8h weights(uint32_t w, uint32_t zero, uint32_t one) {
+        const v8h v = Products<WQ_F16>::weights(w, one);
         const v4u z = {zero, zero, zero, zero};
         return v + __builtin_bit_cast(v8h, z);
     }
@@ -41,9 +41,8 @@ template <> struct Exact<WQ_F16> {
 template <> struct Exact<WQ_I8> {
     __device__ static uint32_t zero(int z) { return 0x04040404u * z; }
     // 4 (code - zero) in every byte: 128 + 4 code holds off a borrow, and its sign bit turned takes the 128 off again
-    __device__ static long weights(uint32_t w, uint32_t zero) {
-        const uint32_t even = (((w & 0x3c3c3c3cu) | 0x80808080u) - zero) ^ 0x80808080u;
-        const uint32_t odd = (((rotate_right(w, 4) & 0x3c3c3c3cu) | 0x80808080u) - zero) ^ 0x80808080u;
+    __device__ static long weights(uint32_t w, uint32_t zero, uint32_t one) {
+        const uint32_t field = 0x3c3c3c3cu, even = (((w & field) | one) - zero) ^ one, odd = (((rotate_right(w, 4) & field) | one) - zero) ^ one;
         // even: inputs 0 4 1 5, odd: 2 6 3 7
         const v2u r = {__builtin_amdgcn_perm(odd, even, 0x06040200u), __builtin_amdgcn_perm(odd, even, 0x07050301u)};
         return __builtin_bit_cast(long, r);
@@ -74,6 +73,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int4_tiles_kernel(const typena
     // the last tile of rows ends with the last row: it may share rows with the one before, which get the same values twice
     const int m0 = max(min(row_tile * kRows, o.M - kRows), 0), n_tile0 = (column * kWaves + wave) * NT;
     const bool fits = matches(w);
+    const uint32_t one = in_lanes(P::kOne);
     auto output_tile = [&](int nt) { return (size_t)min(n_tile0 + nt, w.output_tiles - 1); };
 
     auto fetch_codes = [&](int kt) {
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int4_tiles_kernel(const typena
                 const uint32_t zero = E::zero(ZEROS ? (int)now.zeros[nt] : 8);
                 const uint32_t* const words = reinterpret_cast<const uint32_t*>(&codes[wave][nt][lane]) + group * kSteps;
 #pragma unroll
-                for (int j = 0; j < kSteps; ++j) ws[nt][j] = E::weights(words[j], zero);
+                for (int j = 0; j < kSteps; ++j) ws[nt][j] = E::weights(words[j], zero, one);
             }
             __builtin_amdgcn_sched_barrier(0);   // the codes are read before the next ones are asked for in their place
             if (group == kGroups - 1 && kt + 1 < w.input_tiles) fetch_codes(kt + 1);
@@ -202,7 +202,6 @@ template <int XT, int GROUP, bool ZEROS, bool BF16, int NT>
 hipError_t launch(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
     const int row_tiles = ceil_div(o.M, kRows);
     const long long tiles = (long long)row_tiles * ceil_div(w.output_tiles, kWaves * NT);
-    if (tiles > (1 << 23)) return hipErrorInvalidValue;
     int4_tiles_kernel<XT, GROUP, ZEROS, BF16, NT><<<(unsigned)tiles, 64 * kWaves, 0, s>>>(static_cast<const typename Element<XT>::type*>(x), x_stride, w, o,
                                                                                         row_tiles, (int)tiles);
     return hipGetLastError();

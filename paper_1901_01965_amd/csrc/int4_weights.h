@@ -59,12 +59,10 @@ __device__ inline bool matches(const Int4Weights& w) {
            (h->scale_type == w.scale_type) & (h->has_zeros == w.has_zeros);
 }
 
-// (w & mask) | bits in one instruction, for which a constant each has to lie in a scalar and a vector register.
-__device__ inline uint32_t masked(uint32_t w, uint32_t mask, uint32_t bits) {
-    uint32_t r;
-    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(w), "s"(mask), "v"(bits));
-    return r;
-}
+// A constant in a vector register, as the compiler sees it a value of each lane: (w & field) | this is one instruction only where not
+// both come from scalar registers.  (Written as inline assembly, that instruction may overwrite the start value of a product under way:
+// the compiler keeps the wait states in between only for instructions that it knows.)
+__device__ inline uint32_t in_lanes(uint32_t constant) { return __builtin_amdgcn_mbcnt_hi(0u, constant); }
 
 __device__ inline uint32_t rotate_right(uint32_t w, int bits) { return __builtin_amdgcn_alignbit(w, w, bits); }
 
@@ -78,9 +76,10 @@ template <> struct Products<WQ_F16> {
     typedef v4f Sum;
     static constexpr float kUnit = 16.0f;   // operand 1 + u / 16
     static constexpr int kOffset = 16;
-    __device__ static Fragment weights(uint32_t w) {
-        const uint32_t field = 0x03c003c0u, one = 0x3c003c00u;
-        const v4u r = {masked(w << 4, field, one), masked(w, field, one), masked(w >> 4, field, one), masked(rotate_right(w, 8), field, one)};
+    static constexpr uint32_t kOne = 0x3c003c00u;
+    __device__ static Fragment weights(uint32_t w, uint32_t one) {   // one: kOne in the lanes
+        const uint32_t field = 0x03c003c0u;
+        const v4u r = {((w << 4) & field) | one, (w & field) | one, ((w >> 4) & field) | one, (rotate_right(w, 8) & field) | one};
         return __builtin_bit_cast(Fragment, r);
     }
     // the same value in every place: -(16 + 8) / 16 where the zero point is 8 everywhere, else -1 / 16
@@ -101,9 +100,10 @@ template <> struct Products<WQ_BF16> {
     typedef v4f Sum;
     static constexpr float kUnit = 16.0f;
     static constexpr int kOffset = 16;
-    __device__ static Fragment weights(uint32_t w) {
-        const uint32_t field = 0x00780078u, one = 0x3f803f80u;
-        const v4u r = {masked(w << 1, field, one), masked(w >> 3, field, one), masked(w >> 7, field, one), masked(rotate_right(w, 11), field, one)};
+    static constexpr uint32_t kOne = 0x3f803f80u;
+    __device__ static Fragment weights(uint32_t w, uint32_t one) {
+        const uint32_t field = 0x00780078u;
+        const v4u r = {((w << 1) & field) | one, ((w >> 3) & field) | one, ((w >> 7) & field) | one, (rotate_right(w, 11) & field) | one};
         return __builtin_bit_cast(Fragment, r);
     }
     __device__ static Fragment ones(bool zeros) {
@@ -123,7 +123,8 @@ template <> struct Products<WQ_I8> {
     typedef v4i Sum;
     static constexpr float kUnit = 0.25f;   // operand 4 u: fields two bits up in their bytes
     static constexpr int kOffset = 0;
-    __device__ static Fragment weights(uint32_t w) {
+    static constexpr uint32_t kOne = 0x80808080u;
+    __device__ static Fragment weights(uint32_t w, uint32_t) {
         const v2u r = {w & 0x3c3c3c3cu, rotate_right(w, 4) & 0x3c3c3c3cu};
         return __builtin_bit_cast(Fragment, r);
     }
@@ -145,10 +146,10 @@ template <> struct Products<WQ_I8> {
 
 // Eight inputs of a row from `k` on, zeros behind the row's end.
 template <int XT>
-__device__ inline auto load_inputs(const typename Element<XT>::type* row, int k, int K, bool whole) {
+__device__ inline auto load_inputs(const typename Element<XT>::type* row, int k, int K) {
     typedef typename Element<XT>::type T;
     typedef std::conditional_t<XT == WQ_I8, v2u, v4u> Bits;
-    if (whole || k + 8 <= K) return load_unaligned<Bits, sizeof(T)>(row + k);
+    if (k + 8 <= K) return load_unaligned<Bits, sizeof(T)>(row + k);
     union { Bits bits; T e[8]; } r;
     r.bits = Bits{};
 #pragma unroll

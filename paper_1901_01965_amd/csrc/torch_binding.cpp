@@ -389,7 +389,7 @@ PyObject* int4_linear_call(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (a[11] == Py_None) y = at::Tensor(at::detail::empty_cuda(shape, out_dtype, x.device(), std::nullopt));
         void* const yp = data<void>(y);
         void* const s = stream();
-        const ScratchTensor scratch(int4_linear_workspace_bytes(xp, x_type, stride, M, K), x, true);
+        const ScratchTensor scratch(int4_linear_workspace_bytes(xp, x_type, stride, M, N, K), x, true);
         return finish(y, [&] {
             return int4_linear(xp, x_type, stride, x_scale, blob, bias, yp, out_type, M, N, K, group, scale_type, zeros, relu, scratch.p,
                                scratch.bytes, s);

@@ -32,7 +32,7 @@ def load_quantized():
         sigs = {
             "int4_packed_bytes": (sz, [i] * 4),
             "int4_pack_weights": (i, [vp, vp, i, vp, i, i, i, vp, sz, vp]),
-            "int4_linear_workspace_bytes": (sz, [vp, i, ll, i, i]),
+            "int4_linear_workspace_bytes": (sz, [vp, i, ll, i, i, i]),
             "int4_linear": (i, [vp, i, ll, vp, vp, vp, vp] + [i] * 8 + [vp, sz, vp]),
             "int8_cache_append": (i, [vp, ll, vp, ll, i, i] + cache + batch + [vp]),
             "int8_cache_read": (i, cache + [vp, i, vp, vp, i, vp]),

@@ -66,11 +66,32 @@ def test_every_size_against_64_bits(M, N, K, group, zeros, dtype):
 
 @pytest.mark.parametrize("dtype", [F16, BF16, I8])
 @pytest.mark.parametrize("group,zeros", [(32, False), (64, True), (128, False), (128, True)])
-def test_enough_rows_and_outputs_for_coarser_tiles(group, zeros, dtype):
-    M, N, K = 1101, 8200, 384
+@pytest.mark.parametrize("M,N,K", [(1101, 8200, 384), (131, 11001, 136), (40, 36001, 129), (300, 5003, 1000)])
+def test_enough_rows_and_outputs_for_tiles(M, N, K, group, zeros, dtype):
+    """The first is large enough for the coarser tiles, the others end inside tiles of rows, outputs and inputs."""
     x, codes, scales, zero = make(M, N, K, group, dtype, zeros, seed=2)
     got = wg.int4_linear(x, wg.pack_int4_weights(codes, scales, zero, group))
     check(got, *reference(x, codes, scales, zero, group), dtype, K, group)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_many_rows_beside_each_other_and_of_unlike_sizes(dtype):
+    """bfloat16 rows are held as float16 with a power of two each: rows of any size, an infinite and a NaN row, strided rows."""
+    M, N, K, group = 300, 5120, 256, 64
+    x, codes, scales, zero = make(M, N, K, group, dtype, True, seed=9)
+    if dtype == BF16:
+        x = (x.float() * 2.0 ** torch.randint(-60, 60, (M, 1), device="cuda")).to(BF16)
+        x[5] = 0
+    packed = wg.pack_int4_weights(codes, scales, zero, group)
+    clean = wg.int4_linear(x, packed, out_dtype=F32)
+    check(clean, *reference(x, codes, scales, zero, group), dtype, K, group)
+    wide = torch.full((M, K + 8), float("nan"), dtype=dtype, device="cuda")
+    wide[:, :K] = x
+    wide[7, 5], wide[200, 0] = float("nan"), float("inf")
+    got = wg.int4_linear(wide[:, :K], packed, out_dtype=F32)
+    rest = [m for m in range(M) if m not in (7, 200)]
+    assert torch.equal(got[rest], clean[rest])
+    assert torch.isnan(got[7]).all() and not torch.isfinite(got[200]).any()
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16, I8])

@@ -35,9 +35,9 @@ def test_every_declared_function_is_exported(lib):
 def test_packed_sizes(lib):
     assert wg.int4_packed_bytes(16, 128, 128) == 256 + 1024 + 256            # header, one tile, 16 scales
     assert wg.int4_packed_bytes(17, 129, 32, True) == 256 + 4 * 1024 + 2 * 8 * 16 * 3
-    for bad in ((0, 128, 128), (16, 0, 128), (16, 128, 48), (16, 128, 0), (1 << 27, 1, 32), (1 << 24, 1 << 11, 32)):
+    for bad in ((0, 128, 128), (16, 0, 128), (16, 128, 48), (16, 128, 0), (1 << 27, 1, 32), (1 << 22, 1 << 13, 32)):
         assert wg.int4_packed_bytes(*bad) == 0
-    assert wg.int4_packed_bytes(1 << 24, 1 << 10, 128) > 1 << 33
+    assert wg.int4_packed_bytes(1 << 22, 1 << 12, 128) > 1 << 33
 
 
 p = ctypes.c_void_p
@@ -66,14 +66,17 @@ def test_products_are_refused_before_any_launch(lib):
     assert call(x=ODD) == call(y=ODD) == call(y=p(0x30002), y_type=F32) == call(blob=p(0x20080)) == call(bias=p(0x20002)) == EINVAL
     assert call(K=1 << 27, stride=1 << 27) == EUNSUPPORTED
     assert call(M=0, x=None, y=None) == OK
-    assert call(M=1 << 24) == EUNSUPPORTED
-    need = lambda **a: lib.int4_linear_workspace_bytes(*dict(dict(x=A, x_type=BF16, stride=128, M=300, K=128), **a).values())
+    assert call(M=1 << 24) == call(M=1 << 21, N=1 << 17) == EUNSUPPORTED
+    need = lambda **a: lib.int4_linear_workspace_bytes(*dict(dict(x=A, x_type=BF16, stride=128, M=300, N=8192, K=128), **a).values())
     assert need() == 300 * 128 * 2 + 300 * 4
-    assert call(M=300, x_type=BF16) == call(M=300, x_type=BF16, workspace=p(0x40010), size=1 << 40) == EINVAL
-    assert call(M=300, x_type=BF16, workspace=D, size=need() - 1) == ESMALLBUF
-    assert need(M=4) == need(x_type=F16) == need(x_type=F32) == need(M=0) == 0   # few rows; whole, aligned tiles; invalid
-    for copied in (dict(K=120), dict(stride=129), dict(x=p(0x10002)), dict(M=100)):
+    many = dict(M=300, N=8192, x_type=BF16)
+    assert call(**many) == call(workspace=p(0x40010), size=1 << 40, **many) == EINVAL
+    assert call(workspace=D, size=need() - 1, **many) == ESMALLBUF
+    assert need(M=4) == need(N=16) == need(x_type=F16) == need(x_type=F32) == need(M=0) == 0   # few rows; whole, aligned tiles; invalid
+    for copied in (dict(K=120), dict(stride=129), dict(x=p(0x10002))):
         assert need(x_type=F16, **copied) > 0
+    assert need(x_type=F16, M=100, N=20000) == 128 * 128 * 2                                   # a tile's rows
+    assert need(M=4, K=120) == 0 and need(M=4, stride=129) == 4 * 128 * 2                      # few rows: pieces, not tiles
 
 
 def cache_args(**over):

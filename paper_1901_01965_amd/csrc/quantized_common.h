@@ -78,16 +78,17 @@ __device__ inline Sequence sequence_of(const Batch& b, int s) {
 
 // Work items of `unit` rows are dealt to sequences without a table of their sums: sequence s owns the items base(s) ..
 // base(s + 1) - 1 with base(s) = floor(start(s) / unit) + extra * s, which are at least count / unit, rounded up, plus extra - 1.
-// Finds the sequence of an item; starts that fall are read as a clamped search finds them.
+// Finds the sequence of an item, the last 64 candidates at once, one a lane; starts that fall are read as the search finds them.
 __device__ inline int item_base(const Batch& b, int s, int unit, int extra) { return start_of(b, s) / unit + extra * s; }
 __device__ inline int sequence_of_item(const Batch& b, int item, int unit, int extra) {
     int low = 0, high = b.sequences - 1;
-    while (low < high) {
+    while (high - low > 64) {
         const int middle = (low + high + 1) >> 1;
         if (item_base(b, middle, unit, extra) <= item) low = middle;
         else high = middle - 1;
     }
-    return low;
+    const int candidate = low + 1 + (threadIdx.x & 63);
+    return low + __builtin_popcountll(__ballot(candidate <= high && item_base(b, min(candidate, high), unit, extra) <= item));
 }
 inline long long item_count(int rows, int sequences, int unit, int extra) { return rows / unit + (long long)extra * sequences; }
 

@@ -178,3 +178,40 @@ def test_blocks_read_back_as_values(block, dim, dtype):
     want_v = (cache.v[at].float() * cache.v_scale[at][:, :, None, None] * there).transpose(2, 3)
     assert torch.equal(k, want_k.to(dtype)) and torch.equal(v, want_v.to(dtype))
     assert wg.int8_cache_read(cache, ids[:0], dtype)[0].shape == (0, heads, block, dim)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("block,dim", [(16, 64), (128, 128), (128, 256)])
+@pytest.mark.parametrize("news", [1, 5])
+def test_special_numbers_in_blocks_of_every_size(news, block, dim, dtype):
+    """Each head holds another kind of numbers, in one token of a block whose older tokens stay."""
+    heads, length = 5, block // 2 + 5
+    x = torch.randn(news, heads, dim, generator=torch.Generator().manual_seed(4))
+    x[-1, 0] = torch.cat((torch.tensor([127.0]), torch.arange(dim - 1) % 100 - 50.5))   # halves
+    x[:, 1] = 0
+    x[-1, 2, :3] = torch.tensor([float("inf"), float("-inf"), float("nan")])
+    x[:, 3] *= 2.0 ** -24 if dtype == F16 else 2.0 ** -130
+    x[-1, 4] = float("nan")
+    x = x.to(dtype).cuda()
+    cache = random_cache(2, heads, dim, block, 3)
+    cache.k_scale[:, 3] = cache.v_scale[:, 3] = 2.0 ** -140
+    cache.v_scale[:, 0] = 1.0
+    want, table = copy_of(cache), torch.ones(1, 1, dtype=torch.int32, device="cuda")
+    reference_append(x, x, want, table, [length], [0, news])
+    cuda = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    wg.int8_cache_append(x, x, cache, table, cuda([length]), cuda([0, news]) if news > 1 else None)
+    assert equal(cache, want)
+
+
+def test_more_sequences_than_a_wave_has_lanes():
+    heads, dim, block, sequences = 1, 64, 16, 200
+    gen = torch.Generator().manual_seed(8)
+    news = torch.randint(0, 5, (sequences,), generator=gen).tolist()
+    lengths = [n + int(torch.randint(0, 30, (1,), generator=gen)) for n in news]
+    table, on_gpu, starts, begins = batch(lengths, news, block, 600)
+    cache = random_cache(600, heads, dim, block, 6)
+    want = copy_of(cache)
+    k, v = torch.randn(2, begins[-1], heads, dim, generator=gen).to(F16).cuda()
+    reference_append(k, v, want, table, lengths, begins)
+    wg.int8_cache_append(k, v, cache, table, on_gpu, starts)
+    assert equal(cache, want)

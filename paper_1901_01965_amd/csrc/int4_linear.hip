@@ -102,25 +102,62 @@ hipError_t launch_rows_in_order(const void* x, int x_type, bool half, long long 
     return half ? run(std::integral_constant<int, WQ_BF16>(), std::true_type()) : run(std::integral_constant<int, WQ_F16>(), std::false_type());
 }
 
+// Adds up the parts of the inputs, in their order, four outputs a thread.
+__global__ __launch_bounds__(256) void int4_join_kernel(const float* sums, int parts, Int4Weights w, Int4Output o) {
+    const int quads = ceil_div(o.N, 4), i = blockIdx.x * 256 + threadIdx.x, m = i / quads, n = 4 * (i % quads);
+    if (m >= o.M || !matches(w)) return;
+    const size_t each = (size_t)o.M * o.N;
+    const float* const from = sums + (size_t)m * o.N + n;
+    v4f total = {};
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) total += load_unaligned<v4f, 4>(from + p * each);   // up to 12 bytes more than a row
+    store_outputs(o, m, n, total, 1.0f);
+}
+
 // Which kernel a call runs, and what it needs of a workspace: a copy of the rows, and one factor each.
 struct Int4Plan {
     bool many, copy;
-    int padded;
-    size_t factors, total;   // bytes
+    int parts, padded;               // parts of the inputs whose sums are added up at the end
+    size_t factors, sums, total;     // offsets of the factors and of the parts' sums, and all in bytes
 };
-// The kernel for many rows takes about 1.2 us per tile of inputs however few workgroups it has, the one for few rows 2.7e-5 us per 4096
-// inputs of every element of y (float16, 4096 inputs: 38 and 30 us for 256 rows and 4096 outputs, 38 and 43 for 384; 40 and 31 us for 64 rows
-// and 16384 outputs, 41 and 44 for 96).
-constexpr long long kManyElements = 1400000;
+// How long either kernel takes, in us, to about a quarter (measured at 40 to 2048 rows, 160 to 28672 outputs of 300 to 28672 inputs).  For few rows:
+// the products, at two rates by how many workgroups read the same activations, or eight waves' turns of 1 us each through the inputs.
+double rows_time(int M, int N, int K) {
+    const double products = 32.0 * ceil_div(M, 32) * N * K * (N < 16 * kComputeUnits ? 13e-9 : 6.6e-9);
+    return 3.0 + max(products, ceil_div(K, kTileInputs) / 8.0);
+}
+// For many: 1.2 us a tile of inputs as long as no two workgroups share a compute unit, a little less each if they do; parts of the inputs are
+// written, read again and added up by a launch more.  (Their best number, one and the kernel for few rows: 1661 rows, 1024 outputs of 28672
+// inputs 132, 318 and 821 us; 256, 4096 of 4096 24, 38 and 29; 128, 4096 of 14336 29, 120 and 39; but 64, 4096 of 4096 20, 42 and 10.)
+double tiles_time(int M, int N, int K, int parts) {
+    const long long workgroups = (long long)ceil_div(M, kTileRows) * ceil_div(N, 8 * kTileOutputs) * parts;
+    const double at_a_time = workgroups <= kComputeUnits ? 1.0 : 0.9 * ((workgroups + kComputeUnits - 1) / kComputeUnits);
+    const double inputs = (double)ceil_div(ceil_div(K, kTileInputs), parts) * 1.2 * at_a_time;
+    return 3.0 + inputs + (parts > 1 ? 6.0 + 1.3e-6 * parts * M * N : 0.0) + (M < kTileRows ? 4.0 : 0.0);
+}
+constexpr int kMostParts = 32;
 
 Int4Plan plan_int4(const void* x, int x_type, long long x_stride, int M, int N, int K) {
-    Int4Plan p = {M > 32 && (long long)M * N > kManyElements, false, ceil_div(K, kTileInputs) * kTileInputs, 0, 0};
+    Int4Plan p = {false, false, 1, ceil_div(K, kTileInputs) * kTileInputs, 0, 0, 0};
+    if (M > 32) {
+        const long long tiles = (long long)ceil_div(M, kTileRows) * ceil_div(N, 8 * kTileOutputs);
+        double least = tiles_time(M, N, K, 1);
+        for (int parts = 2; parts <= kMostParts && 2 * parts <= ceil_div(K, kTileInputs) && tiles * parts <= 4 * kComputeUnits; ++parts) {
+            const double time = tiles_time(M, N, K, parts);
+            if (time >= least) continue;
+            least = time;
+            p.parts = parts;
+        }
+        p.many = least < rows_time(M, N, K);
+        if (!p.many) p.parts = 1;
+    }
     const size_t size = x_type == WQ_I8 ? 1 : 2;
     // both kernels read whole aligned pieces of rows, the one for many rows also whole tiles only
     p.copy = (x_stride * size) % 16 != 0 || !aligned(x, 16) || x_stride > (1 << 24) || (p.many && (x_type == WQ_BF16 || M < kTileRows || K % kTileInputs != 0));
-    if (!p.copy) return p;
-    p.factors = (((size_t)(p.many ? max(M, kTileRows) : M) * p.padded * size) + 255) & ~(size_t)255;
-    p.total = p.factors + (p.many && x_type == WQ_BF16 ? (size_t)M * sizeof(float) : 0);
+    const auto whole = [](size_t bytes) { return (bytes + 255) & ~(size_t)255; };
+    if (p.copy) p.factors = whole((size_t)(p.many ? max(M, kTileRows) : M) * p.padded * size);
+    p.sums = p.factors + (p.many && x_type == WQ_BF16 ? whole((size_t)M * sizeof(float)) : 0);
+    p.total = p.sums + (p.parts > 1 ? whole((size_t)p.parts * M * N * sizeof(float) + 12) : 0);
     return p;
 }
 
@@ -185,8 +222,15 @@ int int4_linear(const void* x_dev, int x_type, long long x_stride, const float* 
         x_stride = p.padded;
         if (p.many && x_type == WQ_BF16) o.x_scale = factors;
     }
-    const auto launch = p.many ? (x_type == WQ_I8 ? launch_int4_tiles_int8 : launch_int4_tiles_half)
-                      : x_type == WQ_F16 ? launch_int4_rows_half : x_type == WQ_BF16 ? launch_int4_rows_bfloat : launch_int4_rows_int8;
+    if (p.many) {
+        const auto launch = x_type == WQ_I8 ? launch_int4_tiles_int8 : launch_int4_tiles_half;
+        if (p.parts == 1) return status_of(launch(x_dev, x_stride, w, o, 1, s));
+        float* const sums = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + p.sums);
+        if (hipError_t e = launch(x_dev, x_stride, w, Int4Output{nullptr, nullptr, sums, WQ_F32, M, N, 0}, p.parts, s)) return status_of(e);
+        int4_join_kernel<<<(unsigned)(((long long)M * ceil_div(N, 4) + 255) / 256), 256, 0, s>>>(sums, p.parts, w, o);
+        return status_of(hipGetLastError());
+    }
+    const auto launch = x_type == WQ_F16 ? launch_int4_rows_half : x_type == WQ_BF16 ? launch_int4_rows_bfloat : launch_int4_rows_int8;
     return status_of(launch(x_dev, x_stride, w, o, s));
 }
 

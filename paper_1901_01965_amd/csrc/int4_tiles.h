@@ -72,6 +72,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int4_tiles_kernel(const typena
     const int in_band = tile - band * kBand * across, row_tile = band * kBand + in_band % height, column = in_band / height;
     // the last tile of rows ends with the last row: it may share rows with the one before, which get the same values twice
     const int m0 = max(min(row_tile * kRows, o.M - kRows), 0), n_tile0 = (column * kWaves + wave) * NT;
+    // tiles of inputs: all, or a part of them (of few outputs only: more a wave leave no registers for it)
+    const int parts = NT == 2 ? gridDim.y : 1, begin = NT == 2 ? w.input_tiles * blockIdx.y / parts : 0, end = NT == 2 ? w.input_tiles * (blockIdx.y + 1) / parts : w.input_tiles;
     const bool fits = matches(w);
     const uint32_t one = in_lanes(P::kOne);
     auto output_tile = [&](int nt) { return (size_t)min(n_tile0 + nt, w.output_tiles - 1); };
@@ -124,13 +126,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int4_tiles_kernel(const typena
 
     v4f acc[NT][kRowTiles] = {};
     Factors next;
-    fetch_codes(0);
-    fetch(0, even);
-    fetch_factors(next, 0);
+    fetch_codes(begin);
+    fetch(begin, even);
+    fetch_factors(next, begin * kGroups);
     auto multiply = [&](int kt, const Held& held, Held& other) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's share of the tile is there
         __syncthreads();                                   // everyone's is, and the other half has been read
-        if (kt + 1 < w.input_tiles) fetch(kt + 1, other);
+        if (kt + 1 < end) fetch(kt + 1, other);
 #pragma unroll 1
         for (int group = 0; group < kGroups; ++group) {
             typename P::Fragment ws[NT][kSteps];
@@ -143,7 +145,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int4_tiles_kernel(const typena
                 for (int j = 0; j < kSteps; ++j) ws[nt][j] = E::weights(words[j], zero, one);
             }
             __builtin_amdgcn_sched_barrier(0);   // the codes are read before the next ones are asked for in their place
-            if (group == kGroups - 1 && kt + 1 < w.input_tiles) fetch_codes(kt + 1);
+            if (group == kGroups - 1 && kt + 1 < end) fetch_codes(kt + 1);
             v4f scale[NT];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) scale[nt] = scales_of<BF16>(now.scales[nt]);
@@ -186,11 +188,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int4_tiles_kernel(const typena
             __builtin_amdgcn_s_setprio(0);
         }
     };
-    for (int kt = 0; kt < w.input_tiles; kt += 2) {
+    for (int kt = begin; kt < end; kt += 2) {
         multiply(kt, even, odd);
-        if (kt + 1 < w.input_tiles) multiply(kt + 1, odd, even);
+        if (kt + 1 < end) multiply(kt + 1, odd, even);
     }
     if (!fits) return;
+    if (parts > 1) o.y = static_cast<float*>(o.y) + (size_t)blockIdx.y * o.M * o.N;
 #pragma unroll
     for (int mt = 0; mt < kRowTiles; ++mt)
 #pragma unroll
@@ -199,10 +202,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int4_tiles_kernel(const typena
 }
 
 template <int XT, int GROUP, bool ZEROS, bool BF16, int NT>
-hipError_t launch(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
+hipError_t launch(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, int parts, hipStream_t s) {
     const int row_tiles = ceil_div(o.M, kRows);
     const long long tiles = (long long)row_tiles * ceil_div(w.output_tiles, kWaves * NT);
-    int4_tiles_kernel<XT, GROUP, ZEROS, BF16, NT><<<(unsigned)tiles, 64 * kWaves, 0, s>>>(static_cast<const typename Element<XT>::type*>(x), x_stride, w, o,
+    int4_tiles_kernel<XT, GROUP, ZEROS, BF16, NT><<<dim3((unsigned)tiles, parts), 64 * kWaves, 0, s>>>(static_cast<const typename Element<XT>::type*>(x), x_stride, w, o,
                                                                                         row_tiles, (int)tiles);
     return hipGetLastError();
 }
@@ -213,15 +216,15 @@ inline long long rounds(const Int4Weights& w, const Int4Output& o, int nt) {
 }
 
 template <int XT>
-hipError_t launch_tiles_of(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
+hipError_t launch_tiles_of(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, int parts, hipStream_t s) {
     return with_weights(w, [&](auto group, auto zeros, auto bf16) {
         // More tiles of outputs a wave read LDS less often per product, in coarser rounds.  Measured against two, alike in rounds: three
         // 0.82 (float16 in groups of 128, whose operands leave no room for four: 4096 rows through 4096 x 8192 260 against 280 us, 8192
         // through 4096 x 28672 1660 and 1797; but 2048 through 4096 x 4096 80 and 70), four 0.92 (int8 183 and 197, groups of 64 264 and 295).
         constexpr int kMore = XT == WQ_F16 && group() == 128 ? 3 : 4;
         constexpr double kCost = kMore == 3 ? 0.82 * 1.5 : 0.92 * 2;
-        if (rounds(w, o, kMore) * kCost < rounds(w, o, 2)) return launch<XT, group(), zeros(), bf16(), kMore>(x, x_stride, w, o, s);
-        return launch<XT, group(), zeros(), bf16(), 2>(x, x_stride, w, o, s);
+        if (parts == 1 && rounds(w, o, kMore) * kCost < rounds(w, o, 2)) return launch<XT, group(), zeros(), bf16(), kMore>(x, x_stride, w, o, 1, s);
+        return launch<XT, group(), zeros(), bf16(), 2>(x, x_stride, w, o, parts, s);
     });
 }
 

@@ -216,9 +216,10 @@ hipError_t launch_int4_pack(const uint8_t* codes, const void* scales, const uint
 hipError_t launch_int4_rows_half(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s);
 hipError_t launch_int4_rows_bfloat(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s);
 hipError_t launch_int4_rows_int8(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s);
-// Many rows: x holds whole tiles (kTileInputs inputs, kTileRows rows or more) of 16-byte aligned rows.
-hipError_t launch_int4_tiles_half(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s);
-hipError_t launch_int4_tiles_int8(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s);
+// Many rows: x holds whole tiles (kTileInputs inputs, kTileRows rows or more) of 16-byte aligned rows.  parts > 1: that many sums of
+// parts of the inputs, one y of float32 behind the other.
+hipError_t launch_int4_tiles_half(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, int parts, hipStream_t s);
+hipError_t launch_int4_tiles_int8(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, int parts, hipStream_t s);
 
 // Calls launch(group, has zero points, scales are bfloat16), each as a constant, for what the weights are.
 template <class F>

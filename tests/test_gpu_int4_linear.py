@@ -66,7 +66,7 @@ def test_every_size_against_64_bits(M, N, K, group, zeros, dtype):
 
 @pytest.mark.parametrize("dtype", [F16, BF16, I8])
 @pytest.mark.parametrize("group,zeros", [(32, False), (64, True), (128, False), (128, True)])
-@pytest.mark.parametrize("M,N,K", [(1101, 8200, 384), (131, 11001, 136), (40, 36001, 129), (300, 5003, 1000)])
+@pytest.mark.parametrize("M,N,K", [(1101, 8200, 384), (131, 11001, 1100), (100, 20001, 2000), (300, 5003, 1000)])
 def test_enough_rows_and_outputs_for_tiles(M, N, K, group, zeros, dtype):
     """The first is large enough for the coarser tiles, the others end inside tiles of rows, outputs and inputs."""
     x, codes, scales, zero = make(M, N, K, group, dtype, zeros, seed=2)
@@ -74,10 +74,27 @@ def test_enough_rows_and_outputs_for_tiles(M, N, K, group, zeros, dtype):
     check(got, *reference(x, codes, scales, zero, group), dtype, K, group)
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16, I8])
+@pytest.mark.parametrize("group,zeros", [(32, False), (64, True), (128, True)])
+@pytest.mark.parametrize("M,N,K", [(1500, 203, 4096), (1300, 260, 3001)])
+@pytest.mark.parametrize("out_dtype", [F16, F32])
+def test_long_sums_of_few_outputs_in_parts(out_dtype, M, N, K, group, zeros, dtype):
+    x, codes, scales, zero = make(M, N, K, group, dtype, zeros, seed=12)
+    bias = torch.randn(N, device="cuda") * 3
+    x_scale = torch.rand(M, device="cuda") + 0.1 if dtype == I8 else None
+    packed = wg.pack_int4_weights(codes, scales, zero, group)
+    got = wg.int4_linear(x, packed, bias=bias, relu=True, x_scale=x_scale, out_dtype=out_dtype)
+    check(got, *reference(x, codes, scales, zero, group, bias, True, x_scale), dtype, K, group)
+    other = wg.PackedInt4Weights(packed.blob, N, K, group, BF16 if packed.scale_dtype == F16 else F16, zeros)
+    out = torch.full((M, N), 5.0, dtype=out_dtype, device="cuda")
+    wg.int4_linear(x, other, x_scale=x_scale, out=out, out_dtype=out_dtype)
+    assert (out == 5).all()
+
+
 @pytest.mark.parametrize("dtype", [F16, BF16])
 def test_many_rows_beside_each_other_and_of_unlike_sizes(dtype):
     """bfloat16 rows are held as float16 with a power of two each: rows of any size, an infinite and a NaN row, strided rows."""
-    M, N, K, group = 300, 5120, 256, 64
+    M, N, K, group = 300, 5120, 512, 64
     x, codes, scales, zero = make(M, N, K, group, dtype, True, seed=9)
     if dtype == BF16:
         x = (x.float() * 2.0 ** torch.randint(-60, 60, (M, 1), device="cuda")).to(BF16)
@@ -195,6 +212,24 @@ def test_captured_and_replayed_on_another_stream(M):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, wg.int4_linear(x, packed))
+
+
+def test_captured_many_rows_that_are_copied_and_summed_in_parts():
+    M, N, K = 1300, 250, 3000
+    x, codes, scales, zero = make(M, N, K, 128, BF16, True, seed=8)
+    packed = wg.pack_int4_weights(codes, scales, zero, 128)
+    out, again = (torch.empty((M, N), dtype=BF16, device="cuda") for _ in range(2))
+    wg.int4_linear(x, packed, out=out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        wg.int4_linear(x, packed, out=out)
+        wg.int4_linear(x, packed, out=again)
+    for seed in (9, 10, 11):
+        x.copy_(make(M, N, K, 128, BF16, True, seed=seed)[0])
+        out.zero_()
+        graph.replay()
+        want = wg.int4_linear(x, packed)
+        assert torch.equal(out, want) and torch.equal(again, want)
 
 
 def test_refusals():

@@ -68,14 +68,16 @@ def test_products_are_refused_before_any_launch(lib):
     assert call(M=0, x=None, y=None) == OK
     assert call(M=1 << 24) == call(M=1 << 21, N=1 << 17) == EUNSUPPORTED
     need = lambda **a: lib.int4_linear_workspace_bytes(*dict(dict(x=A, x_type=BF16, stride=128, M=300, N=8192, K=128), **a).values())
-    assert need() == 300 * 128 * 2 + 300 * 4
+    assert need() == 300 * 128 * 2 + 1280                                                      # rows, and 300 factors in whole 256 bytes
     many = dict(M=300, N=8192, x_type=BF16)
     assert call(**many) == call(workspace=p(0x40010), size=1 << 40, **many) == EINVAL
     assert call(workspace=D, size=need() - 1, **many) == ESMALLBUF
     assert need(M=4) == need(N=16) == need(x_type=F16) == need(x_type=F32) == need(M=0) == 0   # few rows; whole, aligned tiles; invalid
     for copied in (dict(K=120), dict(stride=129), dict(x=p(0x10002))):
         assert need(x_type=F16, **copied) > 0
-    assert need(x_type=F16, M=100, N=20000) == 128 * 128 * 2                                   # a tile's rows
+    assert need(x_type=F16, M=100, N=20000, K=2048, stride=2048) == 128 * 2048 * 2             # a tile's rows
+    parts, rest = divmod(need(x_type=F16, M=1500, N=203, K=4096, stride=4096) - 256, 1500 * 203 * 4)
+    assert parts > 1 and rest <= 12                                                            # few outputs, long sums
     assert need(M=4, K=120) == 0 and need(M=4, stride=129) == 4 * 128 * 2                      # few rows: pieces, not tiles
 
 

@@ -16,7 +16,7 @@ struct AttentionArgs {
     int kv_heads, group;               // heads of queries per head of keys
     int tile_rows, unit, head_tiles;   // a workgroup's rows: up to `unit` of a sequence's, of a group's heads or tile_rows of them
     int causal, window;
-    int splits, least_steps;           // parts of a sequence at the most, steps of a part at the least
+    int splits, least_steps;           // parts of a sequence at the most, steps of a part at the least (about)
     float scale_log2, sign;            // |scale| / ln 2: exponentials are taken to base 2
 };
 
@@ -81,7 +81,7 @@ __device__ inline bool tile_of(const AttentionArgs& a, int item, int y, Tile& t)
     visible(a, position + t.tokens - 1, t.sequence.length, t.low_all, t.high);
     t.begin = t.low & ~(kStep - 1);
     t.steps = max(ceil_div(t.high - t.begin, kStep), 0);
-    t.per = ceil_div(t.steps, min(a.splits, max(t.steps / a.least_steps, 1)));
+    t.per = ceil_div(t.steps, min(a.splits, max((t.steps + a.least_steps / 2) / a.least_steps, 1)));
     return true;
 }
 

@@ -74,14 +74,19 @@ AttentionPlan plan_attention(int rows, int heads, int kv_heads, int head_dim, in
         while (has_starts && 2 * p.unit * group <= 16) p.unit *= 2;
     p.items = has_starts ? item_count(rows, sequences, p.unit, 1) : sequences;
     const long long tiles = p.items * kv_heads * p.head_tiles;
-    // Few tiles: as many parts as give every compute unit a workgroup (two with many rows), of at least one step for each wave.  Enough
-    // tiles: four parts each, of at least two steps for each wave, so that what is left of the longest sequences at the end is small
-    // (64 sequences, 8 heads of keys, 500 to 8192 tokens: 140 us unsplit, 127 so; one of 30000 among 1500: 358 and 126; all of 4096: 102
-    // and 113).
+    // Few rows, few tiles: as many parts as give every compute unit a workgroup, but none a second (11 sequences of 1550 tokens, 8 heads of 256:
+    // 28 us in 2 parts, 38 in 3), of about one step for each wave.  Enough tiles: four parts each, of about two steps for each wave, so that
+    // what is left of the longest sequences at the end is small (64 sequences, 8 heads of keys, 500 to 8192 tokens: 140 us unsplit, 127
+    // so; one of 30000 among 1500: 358 and 126; all of 4096: 102 and 113).
+    // Many rows: as many as give every compute unit two workgroups, but none a third, of eight steps, since a part's sums go through
+    // memory; two parts, which gain least, of 32 (5 heads of keys, 4 of queries each, 353 rows at 4381 tokens: 147 us unsplit, 47 in 8
+    // parts, 57 in 9; 600 rows at 600 tokens: 29 unsplit, 36 in parts of four steps; 8 heads, 1024 at 1024: 43 and 58 in 2 of eight).
     const bool enough = !p.many && tiles >= kComputeUnits;
-    p.least_steps = enough ? 8 : 4;
-    const long long most = min(max((long long)width * block / (kStep * p.least_steps), 1ll), (long long)kMostParts);
-    p.splits = (int)min(enough ? 4ll : ((p.many ? 2ll : 1ll) * kComputeUnits + tiles - 1) / tiles, most);
+    const long long likely = max(((long long)ceil_div(rows, p.unit) + (sequences - 1) / 2) * kv_heads, 1ll);   // tiles that have rows
+    const long long wanted = enough ? 4 : p.many ? max(2 * kComputeUnits / likely, 1ll) : max(kComputeUnits / tiles, 1ll);
+    p.least_steps = p.many ? (wanted > 2 ? 8 : 32) : enough ? 8 : 4;
+    const long long most = min(max(((long long)width * block / kStep + p.least_steps / 2) / p.least_steps, 1ll), (long long)kMostParts);
+    p.splits = (int)min(wanted, most);
     p.workspace = p.splits > 1 ? (size_t)tiles * p.splits * p.tile_rows * (head_dim + 2) * sizeof(float) : 0;
     return p;
 }

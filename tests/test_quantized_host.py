@@ -76,8 +76,8 @@ def test_products_are_refused_before_any_launch(lib):
     for copied in (dict(K=120), dict(stride=129), dict(x=p(0x10002))):
         assert need(x_type=F16, **copied) > 0
     assert need(x_type=F16, M=100, N=20000, K=2048, stride=2048) == 128 * 2048 * 2             # a tile's rows
-    parts, rest = divmod(need(x_type=F16, M=1500, N=203, K=4096, stride=4096) - 256, 1500 * 203 * 4)
-    assert parts > 1 and rest <= 12                                                            # few outputs, long sums
+    parts, rest = divmod(need(x_type=F16, M=1500, N=203, K=4096, stride=4096), 1500 * 203 * 4)
+    assert parts > 1 and rest < 268                                                            # few outputs, long sums
     assert need(M=4, K=120) == 0 and need(M=4, stride=129) == 4 * 128 * 2                      # few rows: pieces, not tiles
 
 

@@ -37,18 +37,27 @@ struct Quantiser {
         inverse = s > 0.0f ? 1.0f / s : 0.0f;
         half = s == 0.0f ? 1.0f : up > 1.0f ? 0.0f : 0.5f * s;
     }
-    // The code of a magnitude up to 127 s in the first byte, the right one if `left`, the most that any value leaves, stays below half.
-    __device__ uint32_t candidate(float x, float& left) const {
-        const float t = __builtin_fmaf(x, inverse, kRounding);
-        left = fmaxf(left, fabsf(__builtin_fmaf(kRounding - t, s, x)));
-        return __builtin_bit_cast(uint32_t, t);
-    }
     __device__ int code(float x) const {
         x *= up;
         float q = rintf(x * inverse);
         const float twice = 2.0f * fabsf(__builtin_fmaf(-q, s, x)), rest = __builtin_fmaf(-q, s, x);
         if (twice > s || (twice == s && ((int)q & 1))) q += rest < 0.0f ? -1.0f : 1.0f;
         return s > 0.0f ? min(max((int)q, -127), 127) : 0;
+    }
+    // The codes of magnitudes up to 127 s, in the first bytes: the candidates, where each leaves less than half of s.  (Short fractions divided by
+    // 127th parts of others come close to halves often: one of 20000 random bfloat16 needs the longer way.)
+    template <int COUNT>
+    __device__ void codes(const float (&x)[COUNT], uint32_t (&c)[COUNT]) const {
+        float left = 0.0f;
+#pragma unroll
+        for (int j = 0; j < COUNT; ++j) {
+            const float t = __builtin_fmaf(x[j], inverse, kRounding);
+            left = fmaxf(left, fabsf(__builtin_fmaf(kRounding - t, s, x[j])));
+            c[j] = __builtin_bit_cast(uint32_t, t);
+        }
+        if (left < half) return;
+#pragma unroll
+        for (int j = 0; j < COUNT; ++j) c[j] = code(x[j]);
     }
 };
 
@@ -67,6 +76,15 @@ __device__ inline uint32_t rescaled4(uint32_t codes, double from, double to, dou
     for (int i = 0; i < 4; ++i) r |= (uint32_t)(rescaled((int8_t)(codes >> (8 * i)), from, to, inverse) & 255) << (8 * i);
     return r;
 }
+
+// Sixteen codes.
+__device__ inline v4u rescaled16(const v4u& codes, double from, double to, double inverse) {
+    return v4u{rescaled4(codes[0], from, to, inverse), rescaled4(codes[1], from, to, inverse), rescaled4(codes[2], from, to, inverse),
+               rescaled4(codes[3], from, to, inverse)};
+}
+
+// The first n bytes of a dword, of none up to all.
+__device__ inline uint32_t first_bytes(int n) { return n <= 0 ? 0u : n >= 4 ? ~0u : (1u << (8 * n)) - 1; }
 
 struct AppendArgs {
     const void* rows[2];
@@ -107,43 +125,43 @@ __global__ __launch_bounds__(kThreads) void int8_append_one_kernel(AppendArgs a)
     if (d < D) codes[is_v ? (d << b.shift) + slot : slot * D + d] = (int8_t)Quantiser(scale).code(as_float<TYPE>(x));
     if (slot == 0 || scale <= old) return;
     const double from = old, to = scale, inverse = 1.0 / to;
+    v4u* const pieces = reinterpret_cast<v4u*>(codes);
     if (!is_v) {
-        for (int e = d; e < slot * (D / 4); e += kThreads) {
-            uint32_t* const p = reinterpret_cast<uint32_t*>(codes) + e;
-            *p = rescaled4(*p, from, to, inverse);
-        }
+        for (int e = d; e < slot * (D / 16); e += kThreads) pieces[e] = rescaled16(pieces[e], from, to, inverse);
         return;
     }
-    const int quads = P / 4;
-    for (int e = d; e < D * quads; e += kThreads) {
-        const int older = slot - 4 * (e & (quads - 1));   // bytes of the dword that are
+    __syncthreads();   // the new codes, which lie between older ones, are there
+    for (int e = d; e < D * P / 16; e += kThreads) {
+        const int older = slot - 16 * (e & (P / 16 - 1));   // bytes of the piece that are
         if (older <= 0) continue;
-        uint32_t* const p = reinterpret_cast<uint32_t*>(codes) + e;
-        const uint32_t word = rescaled4(*p, from, to, inverse);
-        if (older >= 4) *p = word;
-        else
-            for (int i = 0; i < older; ++i) reinterpret_cast<int8_t*>(p)[i] = (int8_t)(word >> (8 * i));
+        const v4u all = pieces[e];
+        v4u r = rescaled16(all, from, to, inverse);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = (r[i] & first_bytes(older - 4 * i)) | (all[i] & ~first_bytes(older - 4 * i));
+        pieces[e] = r;
     }
 }
 
 // The last tokens of sequences, many of each: one workgroup per block that receives tokens and head, keys and values apart.  A thread holds four tokens by eight channels (up to four
 // times) in registers as they come: their largest magnitude, by their bits, gives the scale, then they become codes.  Keys are stored
 // as they lie.  Values change places between tokens and channels, through LDS by dwords of four tokens, channel 8 p + j in row
-// j D / 8 + p there, which keeps the writes free of bank conflicts; of a dword that also holds bytes that are to stay only the others
-// are stored.
+// j D / 8 + p there, which keeps the writes free of bank conflicts; 16 bytes that also hold some that are to stay are read first and
+// stored with them.
 //
-// Bound by the bytes of the new tokens (11000 tokens, 8 heads of 128, blocks of 32: 21 us, 3.2 TB/s in and out; 34 with the tokens read
+// Bound by the bytes of the new tokens (11000 tokens, 8 heads of 128, blocks of 32: 18 us, 3.7 TB/s in and out; 34 with the tokens read
 // twice and every quotient corrected).
 template <int TYPE, int D, int P>
 __global__ __launch_bounds__(kThreads) void int8_append_kernel(AppendArgs a) {
     constexpr int kPieces = D / 8;                            // of a row
     constexpr int kUnits = P / 4 * kPieces, kAThread = (kUnits + kThreads - 1) / kThreads;
+    constexpr int kUsed = kUnits < 64 ? 64 : kUnits < kThreads ? kUnits : kThreads;
+    constexpr int kRest = (D * P / 16 + kUsed - 1) / kUsed;   // 16-byte pieces of the block that a thread has
     constexpr int kLine = P / 4 + 1;                          // dwords of a row of turned
     __shared__ uint32_t wave_largest[2][kThreads / 64];
     __shared__ uint32_t turned[D * kLine];
 
     const Batch& b = a.batch;
-    const int item = blockIdx.x, head = blockIdx.y, is_v = blockIdx.z, threads = min(kThreads, max(kUnits, 64));
+    const int item = blockIdx.x, head = blockIdx.y, is_v = blockIdx.z;
     const int s = sequence_of_item(b, item, P, 2);
     const Sequence q = sequence_of(b, s);
     const long long base = (long long)q.length - q.count;   // position of the first row
@@ -184,7 +202,7 @@ __global__ __launch_bounds__(kThreads) void int8_append_kernel(AppendArgs a) {
         for (int step = 32; step > 0; step >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, step));
         if ((threadIdx.x & 63) == 0) of_waves[threadIdx.x >> 6] = m;
         __syncthreads();
-        for (int w = 0; w < threads / 64; ++w) m = max(m, of_waves[w]);
+        for (int w = 0; w < kUsed / 64; ++w) m = max(m, of_waves[w]);
         return m;
     };
     uint32_t most = largest(wave_largest[0]);   // and nobody stores the scale before all have read it
@@ -205,70 +223,69 @@ __global__ __launch_bounds__(kThreads) void int8_append_kernel(AppendArgs a) {
     for (int i = 0; i < kAThread; ++i) {
         const int quad = quad_of(i);
         if (!takes_part(quad)) continue;
-        float left = 0.0f;
-        const auto code = [&](int t, int j) { return quantiser.candidate(as_float<TYPE>(bits[i][t][j]), left); };
-        uint32_t* const column = turned + piece * kLine + quad;   // channel j of the eight is j * kPieces rows on
         // (each branch is to hold what it needs in turn: what both begin with is not to be done before them)
         if (!is_v) {
             asm volatile("; keys");
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                const v2u packed = {bytes_of(code(t, 0), code(t, 1), code(t, 2), code(t, 3)), bytes_of(code(t, 4), code(t, 5), code(t, 6), code(t, 7))};
+                float x[8];
+                uint32_t c[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = as_float<TYPE>(bits[i][t][j]);
+                quantiser.codes(x, c);
                 const int token = 4 * quad + t;
-                if (token >= lo && token < hi) *reinterpret_cast<v2u*>(codes + token * D + piece * 8) = packed;
+                if (token >= lo && token < hi)
+                    *reinterpret_cast<v2u*>(codes + token * D + piece * 8) = v2u{bytes_of(c[0], c[1], c[2], c[3]), bytes_of(c[4], c[5], c[6], c[7])};
             }
         } else {
             asm volatile("; values");
 #pragma unroll
-            for (int j = 0; j < 8; ++j) column[j * kPieces * kLine] = bytes_of(code(0, j), code(1, j), code(2, j), code(3, j));
-        }
-        if (left < quantiser.half) continue;
-        // a candidate may be wrong, about once in a million values: the thread's once more
-#pragma unroll 1
-        for (int t = 0; t < 4; ++t) {
-            const int token = 4 * quad + t;
-            v4u x = __builtin_bit_cast(v4u, finite<TYPE>(load_unaligned<v8s, 2>(values_of(token))));
-#pragma unroll 1
             for (int j = 0; j < 8; ++j) {
-                const int8_t c = (int8_t)quantiser.code(as_float<TYPE>((uint16_t)x[0]));
-                if (is_v) reinterpret_cast<int8_t*>(column + j * kPieces * kLine)[t] = c;
-                else if (token >= lo && token < hi) codes[token * D + piece * 8 + j] = c;
-                x = v4u{__builtin_amdgcn_alignbit(x[1], x[0], 16), __builtin_amdgcn_alignbit(x[2], x[1], 16), __builtin_amdgcn_alignbit(x[3], x[2], 16), x[3] >> 16};
+                float x[4];
+                uint32_t c[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) x[t] = as_float<TYPE>(bits[i][t][j]);
+                quantiser.codes(x, c);
+                turned[(j * kPieces + piece) * kLine + quad] = bytes_of(c[0], c[1], c[2], c[3]);
             }
         }
     }
     const double from = old, to = scale, inverse = grown ? 1.0 / to : 0.0;
+    v4u* const pieces = reinterpret_cast<v4u*>(codes);
+    v4u older[kRest];
+    const auto piece_of = [](int i) { return (int)threadIdx.x + i * kUsed; };
     if (!is_v) {
-        if (grown)
-            for (int e = threadIdx.x; e < lo * (D / 4); e += threads) {
-                uint32_t* const p = reinterpret_cast<uint32_t*>(codes) + e;
-                *p = rescaled4(*p, from, to, inverse);
-            }
+        if (!grown) return;
+#pragma unroll
+        for (int i = 0; i < kRest; ++i)
+            if (piece_of(i) < lo * (D / 16)) older[i] = pieces[piece_of(i)];
+#pragma unroll
+        for (int i = 0; i < kRest; ++i)
+            if (piece_of(i) < lo * (D / 16)) pieces[piece_of(i)] = rescaled16(older[i], from, to, inverse);
         return;
+    }
+    const int begin = grown ? 0 : lo;   // bytes begin .. hi - 1 of every channel change
+    const auto token_of = [&](int i) { return piece_of(i) % (P / 16) * 16; };
+    const auto changes = [&](int i) { return piece_of(i) < D * P / 16 && token_of(i) < hi && token_of(i) + 16 > begin; };
+#pragma unroll
+    for (int i = 0; i < kRest; ++i) {
+        older[i] = v4u{};
+        if (changes(i) && (token_of(i) < lo || token_of(i) + 16 > hi)) older[i] = pieces[piece_of(i)];
     }
     __syncthreads();
-    const auto row_of = [](int d) { return (d % 8 * kPieces + d / 8) * kLine; };
-    if (lo == 0 && hi == P) {
-        for (int e = threadIdx.x; e < D * (P / 16); e += threads) {
-            const uint32_t* const from = &turned[row_of(e / (P / 16)) + e % (P / 16) * 4];
-            reinterpret_cast<v4u*>(codes)[e] = v4u{from[0], from[1], from[2], from[3]};
+#pragma unroll
+    for (int i = 0; i < kRest; ++i) {
+        if (!changes(i)) continue;
+        const int d = piece_of(i) / (P / 16), token = token_of(i);
+        const uint32_t* const from_lds = &turned[(d % 8 * kPieces + d / 8) * kLine + token / 4];
+        v4u r = older[i];
+        if (grown && token < lo) r = rescaled16(older[i], from, to, inverse);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t before = first_bytes(lo - token - 4 * j), until = first_bytes(hi - token - 4 * j);
+            r[j] = (r[j] & before) | (from_lds[j] & until & ~before) | (older[i][j] & ~until);
         }
-        return;
-    }
-    const int begin = grown ? 0 : lo;   // bytes begin .. hi - 1 of every row change
-    const int first_quad = begin / 4, count = (hi + 3) / 4 - first_quad;
-    for (int e = threadIdx.x; e < D * count; e += threads) {
-        const int d = e / count, quad = first_quad + e % count;
-        uint32_t* const p = reinterpret_cast<uint32_t*>(codes + d * P) + quad;
-        uint32_t word = 4 * quad + 3 >= lo ? turned[row_of(d) + quad] : 0;
-        if (4 * quad < lo && grown) {
-            const uint32_t older = rescaled4(*p, from, to, inverse), keep = lo - 4 * quad >= 4 ? ~0u : (1u << (8 * (lo - 4 * quad))) - 1;
-            word = (older & keep) | (word & ~keep);
-        }
-        if (4 * quad >= begin && 4 * quad + 4 <= hi) *p = word;
-        else
-            for (int i = 0; i < 4; ++i)
-                if (4 * quad + i >= begin && 4 * quad + i < hi) reinterpret_cast<int8_t*>(p)[i] = (int8_t)(word >> (8 * i));
+        pieces[piece_of(i)] = r;
     }
 }
 

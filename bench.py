@@ -238,6 +238,24 @@ def run_stack(args):
     same = bool(torch.equal(final, acts[13]))
     direct_ms, _ = timed(direct_step, 10)
     same_direct = bool(torch.equal(final, acts[13])) if mode == wg.LOSSLESS else None
+    classified = None
+    if args.classifier:
+        head = [packed_int4(torch, wg, n, k, torch.float16, i) for i, (n, k) in enumerate(wl.VGG16_CLASSIFIER)]
+        row_scale = torch.full((batch,), 1.0 / 32, device=dev)
+
+        def classify():
+            h = wg.int4_linear(acts[13].view(batch, -1), head[0], relu=True, x_scale=row_scale, out_dtype=torch.float16)
+            return wg.int4_linear(wg.int4_linear(h, head[1], relu=True), head[2])
+
+        def both():
+            step()
+            classify()
+
+        both_ms, _ = timed(both, steps)
+        head_ms, _ = timed(classify, steps)
+        classified = {"stack_and_classifier_ms": round(both_ms, 4), "classifier_ms": round(head_ms, 4),
+                      "outputs_by_inputs": wl.VGG16_CLASSIFIER, "finite": bool(torch.isfinite(classify()).all().item())}
+        step()
     print(json.dumps({
         "metric": "direct-equivalent int8 conv TOPS, VGG-16-shaped stack, 1 GPU", "value": round(ops / (ms * 1e-3) / 1e12, 2),
         "unit": "TOPS", "n_gpus": 1, "steps": steps, "warmup": args.warmup, "ms_per_step": round(ms, 4),
@@ -246,10 +264,69 @@ def run_stack(args):
                                "(power-of-two requantisation, ReLU, 2x2 max-pool after layers 2,4,7,10,13)" % (batch, args.mode)},
         "launch": ("hip graph of %d steps: untimed replays for %d ms, then one timed replay" % (steps, SETTLE_MS)
                    if graphed else "eager"),
-        "layers": layers,
+        "layers": layers, **({"classifier": classified} if classified else {}),
         "int32_conv_plus_requant_kernel_ms": round(two_ms, 4), "final_activations_equal": same,
         "direct_conv_plus_requant_kernel_ms": round(direct_ms, 4), "final_activations_equal_direct": same_direct,
         "nonzero_fraction_of_final_activations": round(float((final != 0).float().mean().item()), 3),
+    }))
+
+
+def packed_int4(torch, wg, outputs, inputs, dtype, seed):
+    """Synthetic 4-bit weights that keep a row's size: codes round(2.5 normal) around 8, a scale per 128 inputs."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    codes = (torch.randn(outputs, inputs, device="cuda", generator=gen) * 2.5).round_().add_(8).clamp_(0, 15).to(torch.uint8)
+    scales = ((torch.rand(outputs, -(-inputs // 128), device="cuda", generator=gen) + 0.5) / (2.5 * inputs ** 0.5)).to(dtype)
+    return wg.pack_int4_weights(codes, scales, group=128)
+
+
+def run_decode(args):
+    """--decode: one token of each of --batch sequences (default 16) with --length tokens in the 8-bit cache through a layer of 4096
+    channels, 32 heads of queries, 8 of keys: projections with 4-bit weights, storing of keys and values, attention, and three more
+    products (4096, 14336 and 4096 outputs)."""
+    import torch
+    import paper_1901_01965_amd as wg
+
+    if not torch.cuda.is_available():
+        sys.exit("bench.py: no GPU visible")
+    torch.cuda.set_device(0)
+    batch, heads, kv_heads, dim, block, inner = args.batch or 16, 32, 8, 128, 64, 14336
+    width = heads * dim
+    shapes = [(width + 2 * kv_heads * dim, width), (width, width), (inner, width), (width, inner)]
+    project, out, up, down = (packed_int4(torch, wg, n, k, torch.bfloat16, i) for i, (n, k) in enumerate(shapes))
+    pages = -(-args.length // block)
+    cache = wg.make_int8_cache(batch * pages, kv_heads, dim, block)
+    cache.k.random_(-127, 128)
+    cache.v.random_(-127, 128)
+    cache.k_scale.fill_(0.02)
+    cache.v_scale.fill_(0.02)
+    table = torch.randperm(batch * pages, device="cuda").to(torch.int32).view(batch, pages)
+    lengths = torch.full((batch,), args.length, dtype=torch.int32, device="cuda")
+    x = torch.randn(batch, width, device="cuda").to(torch.bfloat16)
+    y = torch.empty_like(x)
+
+    def step():
+        q, k, v = wg.int4_linear(x, project).split((width, kv_heads * dim, kv_heads * dim), 1)
+        wg.int8_cache_append(k.view(batch, kv_heads, dim), v.view(batch, kv_heads, dim), cache, table, lengths)
+        a = wg.int8_cache_attention(q.view(batch, heads, dim), cache, table, lengths)
+        h = wg.int4_linear(wg.int4_linear(a.flatten(1), out), up, relu=True)
+        wg.int4_linear(h, down, out=y)
+
+    for _ in range(max(1, args.warmup)):
+        step()
+    torch.cuda.synchronize()
+    ms, graphed = time_replay(torch, step, args.steps, args.eager)
+    # what has to be read: codes and scales of the weights, and of every token's keys and values
+    read = sum(n * k // 2 + n * (k // 128) * 2 for n, k in shapes) + 2 * batch * kv_heads * (args.length * dim + 4 * pages)
+    print(json.dumps({
+        "metric": "tokens/s through one layer, 4-bit weights, 8-bit cache, 1 GPU", "value": round(batch / (ms * 1e-3), 1), "unit": "tokens/s",
+        "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": round(ms, 5), "higher_is_better": True, "scaling": "weak",
+        "vs_baseline": None, "dtype": "bf16", "data": "synthetic",
+        "config": {"workload": "one token of %d sequences of %d tokens, %d channels, %d heads of queries and %d of keys, %d inner channels"
+                               % (batch, args.length, width, heads, kv_heads, inner)},
+        "launch": ("hip graph of %d steps: untimed replays for %d ms, then one timed replay" % (args.steps, SETTLE_MS)
+                   if graphed else "eager"),
+        "bytes_read": read, "GB_per_s": round(read / (ms * 1e-3) / 1e9, 1), "finite": bool(torch.isfinite(y).all().item()),
     }))
 
 
@@ -344,6 +421,11 @@ def main():
                          "waves wherever possible, 2 never")
     ap.add_argument("--stack", action="store_true",
                     help="time the VGG-16-shaped stack (cfg5) instead of one layer; prints its own JSON line")
+    ap.add_argument("--classifier", action="store_true",
+                    help="with --stack: also time the stack with three products with 4-bit weights behind it (4096, 4096 and 1000 outputs)")
+    ap.add_argument("--decode", action="store_true",
+                    help="time one token of every sequence through a layer with 4-bit weights and an 8-bit cache; prints its own JSON line")
+    ap.add_argument("--length", type=int, default=4096, help="with --decode: tokens of a sequence in the cache")
     args = ap.parse_args()
     if args.gpus != 1:
         sys.exit("bench.py: this build measures one GPU only (the path has no cross-GPU step); use --gpus 1")
@@ -355,8 +437,14 @@ def main():
     if args.scaled_variant:
         import paper_1901_01965_amd as wg_
         wg_.scaled_variant(args.scaled_variant)
+    if args.classifier and not args.stack:
+        sys.exit("bench.py: --classifier goes with --stack")
     if args.stack:
         return run_stack(args)
+    if args.decode:
+        if args.length < 1:
+            sys.exit("bench.py: --length is one token or more")
+        return run_decode(args)
     if args.algorithm == "f2x2":
         return run_f2x2(args)
 

@@ -58,6 +58,8 @@ VGG16_LAYERS: List[Tuple[int, int, int, bool]] = [
     (512, 512, 14, False), (512, 512, 14, False), (512, 512, 14, True),
 ]
 VGG16_BATCH = 16
+# the products behind its last maps of 512 x 7 x 7: (outputs, inputs)
+VGG16_CLASSIFIER: List[Tuple[int, int]] = [(4096, 25088), (4096, 4096), (1000, 4096)]
 # Fixed requantisation shifts per layer (harness constants): s = max(0, bitlen(max y) - 7) measured by the CPU
 # oracle on image 0, written by tests/golden/make_vgg16_shifts.py into tests/golden/vgg16_shifts.txt.
 VGG16_SHIFTS = [9, 9, 9, 10, 10, 10, 10, 11, 10, 10, 11, 11, 10]

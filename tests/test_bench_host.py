@@ -36,3 +36,9 @@ def test_matrix_core_work_counts_the_methods_products():
     assert bench.contraction_int8_ops(case, "scaled") == 2 * 112 * pairs
     # the direct method multiplies 144 times per tile and channel pair (16 outputs x 9 taps)
     assert case.direct_ops == 2 * 144 * pairs
+
+
+def test_options_that_do_not_go_together_are_refused():
+    for words, message in ((["--classifier"], "--stack"), (["--decode", "--length", "0"], "one token")):
+        proc = subprocess.run([sys.executable, os.path.join(ROOT, "bench.py"), *words], capture_output=True, text=True)
+        assert proc.returncode != 0 and message in proc.stderr and not proc.stdout.strip()

@@ -11,11 +11,14 @@ namespace {
 // of one read of each.
 constexpr int kJoinRows = 4;
 
+// Workgroups for a tile, of the rows that it can have.
+__host__ __device__ constexpr int join_groups(int unit, int group, int tile_rows) { return (min(unit * min(group, tile_rows), tile_rows) + kJoinRows - 1) / kJoinRows; }
+
 template <int TYPE, int D>
 __global__ __launch_bounds__(64 * kJoinRows) void int8_attention_join_kernel(AttentionArgs a) {
     constexpr int kAcross = D / 4, kDown = 64 / kAcross;
     __shared__ float factors[kJoinRows][kMostParts];
-    const int groups = ceil_div(a.tile_rows, kJoinRows), item = blockIdx.x / groups, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int groups = join_groups(a.unit, a.group, a.tile_rows), item = blockIdx.x / groups, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Tile t;
     if (!tile_of(a, item, blockIdx.y, t)) return;
     const int row = blockIdx.x % groups * kJoinRows + wave;
@@ -51,7 +54,7 @@ __global__ __launch_bounds__(64 * kJoinRows) void int8_attention_join_kernel(Att
 
 template <int TYPE, int D>
 hipError_t join(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) {
-    const long long groups = p.items * ceil_div(p.tile_rows, kJoinRows);
+    const long long groups = p.items * join_groups(p.unit, a.group, p.tile_rows);
     int8_attention_join_kernel<TYPE, D><<<dim3((unsigned)groups, a.kv_heads * a.head_tiles), 64 * kJoinRows, 0, s>>>(a);
     return hipGetLastError();
 }

@@ -179,14 +179,15 @@ __global__ __launch_bounds__(64 * kWaves, WGS) void int8_attention_many_kernel(A
         if (masked) {
             if (hidden || token0 >= wave_high || token0 + kLane <= wave_low) v_scale = 0.0f;   // whatever lies there
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
+            for (int rt = 0; rt < RT; ++rt) {
+                // low <= token < high, in one comparison
+                const uint32_t from = (uint32_t)(token0 - low[rt]), seen = hidden ? 0u : (uint32_t)max(high[rt] - low[rt], 0);
 #pragma unroll
                 for (int part = 0; part < kParts; ++part)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int token = token0 + 4 * part + i;
-                        if (hidden || token < low[rt] || token >= high[rt]) scores[rt][part][i] = -INFINITY;
-                    }
+                    for (int i = 0; i < 4; ++i)
+                        if (from + 4 * part + i >= seen) scores[rt][part][i] = -INFINITY;
+            }
         }
         float top[RT], factor[RT];
         bool grown = v_scale > unit;

@@ -130,13 +130,13 @@ __global__ __launch_bounds__(64 * kWaves) void int8_attention_kernel(AttentionAr
         if (masked) {
             // scales of blocks that no row sees are whatever lies there
             if (now.bad || token0 >= t.high || token0 + 16 <= t.low) v_scale = 0.0f;
+            // low <= token < high, in one comparison
+            const uint32_t from = (uint32_t)(token0 - low), seen = now.bad ? 0u : (uint32_t)max(high - low, 0);
 #pragma unroll
             for (int part = 0; part < 4; ++part)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int token = token0 + 4 * part + i;
-                    if (now.bad || token < low || token >= high) scores[part][i] = -INFINITY;
-                }
+                for (int i = 0; i < 4; ++i)
+                    if (from + 4 * part + i >= seen) scores[part][i] = -INFINITY;
         }
 #pragma unroll
         for (int part = 0; part < 4; ++part)

@@ -41,7 +41,8 @@ size_t int4_linear_workspace_bytes(const void* x_dev, int x_type, long long x_st
 /* x: [M][K] of x_type WQ_F16, WQ_BF16 or WQ_I8, rows x_stride elements apart (x_stride >= K).  x_scale: float [M], only for
  * WQ_I8, or NULL.  bias: float [N] or NULL.  y: dense [M][N] of y_type WQ_F16, WQ_BF16 or WQ_F32.  The blob has to be the one
  * made for these (N, K, group, scale_type, has_zeros); on a mismatch y is left untouched.  A row of x with an infinite or NaN
- * element makes that row of y infinite or NaN.  workspace: int4_linear_workspace_bytes(...) bytes, scratch of this call alone while
+ * element has infinite or NaN sums; so may one whose magnitudes add up to more than 1.7e38 within a group, which bfloat16
+ * allows.  y must not overlap x.  workspace: int4_linear_workspace_bytes(...) bytes, scratch of this call alone while
  * it runs. */
 int int4_linear(const void* x_dev, int x_type, long long x_stride, const float* x_scale_dev, const void* packed_dev,
                 const float* bias_dev, void* y_dev, int y_type, int M, int N, int K, int group, int scale_type, int has_zeros,
@@ -51,7 +52,8 @@ int int4_linear(const void* x_dev, int x_type, long long x_stride, const float* 
  * A cache holds blocks of `block` (16, 32, 64 or 128) tokens of kv_heads heads of head_dim (64, 128 or 256):
  *   k  int8 [blocks][kv_heads][block][head_dim],  k_scale float [blocks][kv_heads]
  *   v  int8 [blocks][kv_heads][head_dim][block],  v_scale float [blocks][kv_heads]
- * a value being code * scale.  Values lie token by token within a head_dim, because attention sums over tokens there.
+ * a value being code * scale, with scales of 0 or more.  Values lie token by token within a head_dim, because attention sums
+ * over tokens there.
  *
  * A batch of sequences is told by table int32 [sequences][table_width] (the blocks of a sequence in order), lengths
  * int32 [sequences] (tokens of a sequence, those of this call included) and starts int32 [sequences + 1]: the rows
@@ -92,7 +94,7 @@ size_t int8_cache_attention_workspace_bytes(int rows, int heads, int kv_heads, i
  * rows q_stride and out_stride elements apart.  A row at position p of its sequence sees the tokens t < lengths[b], where
  * causal is set only t <= p, and where window > 0 only t > p - window (window needs causal).  A row that sees nothing
  * becomes 0, and so does a row in front of its sequence's first token; rows behind starts[sequences] are left as they were.
- * workspace: int8_cache_attention_workspace_bytes(...) bytes, scratch of this call alone while it runs.
+ * out must not overlap q.  workspace: int8_cache_attention_workspace_bytes(...) bytes, scratch of this call alone while it runs.
  */
 int int8_cache_attention(const void* q_dev, long long q_stride, int type, int rows, int heads, const int8_t* cache_k_dev,
                          const int8_t* cache_v_dev, const float* k_scale_dev, const float* v_scale_dev, int blocks, int kv_heads,

@@ -148,12 +148,12 @@ Int4Plan plan_int4(const void* x, int x_type, long long x_stride, int M, int N, 
             least = time;
             p.parts = parts;
         }
-        p.many = least < rows_time(M, N, K);
+        p.many = least < rows_time(M, N, K) || (long long)M * N > 1ll << 30;   // a launch of fewer than 2^32 threads either way
         if (!p.many) p.parts = 1;
     }
     const size_t size = x_type == WQ_I8 ? 1 : 2;
     // both kernels read whole aligned pieces of rows, the one for many rows also whole tiles only
-    p.copy = (x_stride * size) % 16 != 0 || !aligned(x, 16) || x_stride > (1 << 24) || (p.many && (x_type == WQ_BF16 || M < kTileRows || K % kTileInputs != 0));
+    p.copy = (M > 1 && (x_stride * size) % 16 != 0) || !aligned(x, 16) || x_stride > (1 << 24) || (p.many && (x_type == WQ_BF16 || M < kTileRows || K % kTileInputs != 0));
     const auto whole = [](size_t bytes) { return (bytes + 255) & ~(size_t)255; };
     if (p.copy) p.factors = whole((size_t)(p.many ? max(M, kTileRows) : M) * p.padded * size);
     p.sums = p.factors + (p.many && x_type == WQ_BF16 ? whole((size_t)M * sizeof(float)) : 0);

@@ -125,7 +125,8 @@ int int8_cache_attention(const void* q_dev, long long q_stride, int type, int ro
     if (empty) return WG_OK;
     if (!q_dev || !out_dev || !aligned(q_dev, 2) || !aligned(out_dev, 2)) return WG_EINVAL;
     const AttentionPlan p = plan_attention(rows, heads, kv_heads, head_dim, block, table_width, sequences, starts_dev != nullptr);
-    if (p.items * max(p.splits, p.splits > 1 ? p.tile_rows : 1) > kMostItems) return WG_EUNSUPPORTED;
+    // workgroups of either launch, which the kernel for many rows has along one dimension
+    if (p.items * max(p.splits, p.splits > 1 ? p.tile_rows : 1) > kMostItems || (p.many && p.items * kv_heads * p.splits > kMostItems)) return WG_EUNSUPPORTED;
     if (p.workspace > 0) {
         if (!workspace_dev || !aligned(workspace_dev, 256)) return WG_EINVAL;
         if (workspace_bytes < p.workspace) return WG_ESMALLBUF;

@@ -368,6 +368,7 @@ PyObject* int4_linear_call(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor& x = on.tensor(a[0], "x");
         const int x_type = element_type(x.scalar_type());
         if (x_type < 0 || x_type == WQ_F32) fail(PyExc_TypeError, "x must be a tensor of torch.float16, torch.bfloat16 or torch.int8");
+        if (K <= 0) fail(PyExc_ValueError, "weights without inputs");
         if (x.dim() < 1 || x.size(x.dim() - 1) != K) {
             PyErr_Format(PyExc_ValueError, "x does not have %d inputs in its last dimension, which the weights were packed for", K);
             throw PyError();

@@ -108,7 +108,7 @@ def pack_int4_weights(codes, scales, zero_points=None, group=128, blob=None):
 def int4_linear(x, packed, bias=None, relu=False, x_scale=None, out_dtype=None, out=None):
     """relu?( x_scale * x W^T + bias ): x float16, bfloat16 or int8 [..., inputs] (two dimensions may have a row stride,
     others are contiguous), bias float32 [outputs], x_scale float32, one per row, only with int8.  The result [..., outputs]
-    is of out_dtype: by default x's, float32 with int8.  Sums are held in 32 bits and rounded once."""
+    is of out_dtype: by default x's, float32 with int8.  Sums are held in 32 bits and rounded once.  out must not overlap x."""
     if type(packed) is not PackedInt4Weights:
         raise TypeError("int4_linear needs a PackedInt4Weights, got %s" % type(packed).__name__)
     if out_dtype is None:

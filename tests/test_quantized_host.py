@@ -129,6 +129,8 @@ def test_rows_and_sizes_are_refused_before_any_launch(lib):
     assert attention(lib, window=-1) == attention(lib, window=5, causal=0) == EINVAL
     assert attention(lib, scale=float("inf")) == attention(lib, scale=float("nan")) == EINVAL
     assert attention(lib, heads=8194, q_stride=1 << 20, out_stride=1 << 20) == EUNSUPPORTED
+    wide = dict(lib=lib, rows=1 << 25, heads=1024, q_stride=1 << 16, out_stride=1 << 16, batch=dict(starts=D))
+    assert attention(cache=dict(heads=1024), **wide) == EUNSUPPORTED      # more workgroups than a grid's dimension
     long = dict(width=4096)
     need = lib.int8_cache_attention_workspace_bytes(3, 4, 2, 64, 16, 4096, 3, 0)
     assert need > 0
@@ -169,6 +171,7 @@ H, I, F = torch.float16, torch.int32, torch.float32
     (ValueError, lambda: wg.int4_linear(gpu(H, 2, 63), packed())),
     (TypeError, lambda: wg.int4_linear(gpu(H, 2, 64), packed(), out_dtype=torch.int8)),
     (RuntimeError, lambda: wg.int4_linear(gpu(H, 2, 64), packed())),                               # no data pointer
+    (ValueError, lambda: wg.int4_linear(gpu(H, 2, 0), wg.PackedInt4Weights(gpu(torch.uint8, 0), 32, 0, 32, H, False))),
 ])
 def test_products_through_the_extension_are_refused(lib, error, call):
     with pytest.raises(error):

@@ -120,30 +120,34 @@ struct Int4Plan {
     int parts, padded;               // parts of the inputs whose sums are added up at the end
     size_t factors, sums, total;     // offsets of the factors and of the parts' sums, and all in bytes
 };
-// How long either kernel takes, in us, to about a quarter (measured at 40 to 2048 rows, 160 to 28672 outputs of 300 to 28672 inputs).  For few rows:
-// the products, at two rates by how many workgroups read the same activations, or eight waves' turns of 1 us each through the inputs.
+// How long either kernel takes, in us, to about a quarter (measured at 33 to 4000 rows, 16 to 30000 outputs of 32 to 28672 inputs).  For few rows:
+// a workgroup to a compute unit at a time, for 16 or 32 outputs of 32 rows, whose eight waves share the tiles of inputs.
 double rows_time(int M, int N, int K) {
-    const double products = 32.0 * ceil_div(M, 32) * N * K * (N < 16 * kComputeUnits ? 13e-9 : 6.6e-9);
-    return 3.0 + max(products, ceil_div(K, kTileInputs) / 8.0);
+    const int tiles = ceil_div(N, kTileOutputs);
+    const long long workgroups = (long long)ceil_div(M, 32) * (tiles < kComputeUnits ? tiles : ceil_div(tiles, 2));
+    return 2.0 + (workgroups + kComputeUnits - 1) / kComputeUnits * (2.2 + 1.05 * ceil_div(ceil_div(K, kTileInputs), 8));
 }
-// For many: 1.2 us a tile of inputs as long as no two workgroups share a compute unit, a little less each if they do; parts of the inputs are
-// written, read again and added up by a launch more.  (Their best number, one and the kernel for few rows: 1661 rows, 1024 outputs of 28672
-// inputs 132, 318 and 821 us; 256, 4096 of 4096 24, 38 and 29; 128, 4096 of 14336 29, 120 and 39; but 64, 4096 of 4096 20, 42 and 10.)
-double tiles_time(int M, int N, int K, int parts) {
+// For many: 1.2 us a tile of inputs as long as no two workgroups share a compute unit, a little less each if they do; parts of the inputs
+// are written, read again and added up by a launch more, and a copy of the rows is another.  (Their best number, one, and the kernel for few
+// rows: 1661 rows, 1024 outputs of 28672 inputs 132, 318 and 821 us; 256, 4096 of 4096 24, 38 and 29; 128, 4096 of 14336 29, 120 and 39;
+// but 64, 4096 of 4096 20, 42 and 10.)
+double tiles_time(int M, int N, int K, int parts, bool copy) {
     const long long workgroups = (long long)ceil_div(M, kTileRows) * ceil_div(N, 8 * kTileOutputs) * parts;
     const double at_a_time = workgroups <= kComputeUnits ? 1.0 : 0.9 * ((workgroups + kComputeUnits - 1) / kComputeUnits);
     const double inputs = (double)ceil_div(ceil_div(K, kTileInputs), parts) * 1.2 * at_a_time;
-    return 3.0 + inputs + (parts > 1 ? 6.0 + 1.3e-6 * parts * M * N : 0.0) + (M < kTileRows ? 4.0 : 0.0);
+    return 3.0 + inputs + (parts > 1 ? 6.0 + 1.3e-6 * parts * M * N : 0.0) + (copy ? 4.0 : 0.0);
 }
 constexpr int kMostParts = 32;
 
 Int4Plan plan_int4(const void* x, int x_type, long long x_stride, int M, int N, int K) {
     Int4Plan p = {false, false, 1, ceil_div(K, kTileInputs) * kTileInputs, 0, 0, 0};
+    // both kernels read whole aligned pieces of rows, the one for many rows also whole tiles only
+    const bool copy = x_type == WQ_BF16 || M < kTileRows || K % kTileInputs != 0;
     if (M > 32) {
         const long long tiles = (long long)ceil_div(M, kTileRows) * ceil_div(N, 8 * kTileOutputs);
-        double least = tiles_time(M, N, K, 1);
+        double least = tiles_time(M, N, K, 1, copy);
         for (int parts = 2; parts <= kMostParts && 2 * parts <= ceil_div(K, kTileInputs) && tiles * parts <= 4 * kComputeUnits; ++parts) {
-            const double time = tiles_time(M, N, K, parts);
+            const double time = tiles_time(M, N, K, parts, copy);
             if (time >= least) continue;
             least = time;
             p.parts = parts;
@@ -152,8 +156,7 @@ Int4Plan plan_int4(const void* x, int x_type, long long x_stride, int M, int N, 
         if (!p.many) p.parts = 1;
     }
     const size_t size = x_type == WQ_I8 ? 1 : 2;
-    // both kernels read whole aligned pieces of rows, the one for many rows also whole tiles only
-    p.copy = (M > 1 && (x_stride * size) % 16 != 0) || !aligned(x, 16) || x_stride > (1 << 24) || (p.many && (x_type == WQ_BF16 || M < kTileRows || K % kTileInputs != 0));
+    p.copy = (M > 1 && (x_stride * size) % 16 != 0) || !aligned(x, 16) || x_stride > (1 << 24) || (p.many && copy);
     const auto whole = [](size_t bytes) { return (bytes + 255) & ~(size_t)255; };
     if (p.copy) p.factors = whole((size_t)(p.many ? max(M, kTileRows) : M) * p.padded * size);
     p.sums = p.factors + (p.many && x_type == WQ_BF16 ? whole((size_t)M * sizeof(float)) : 0);

@@ -34,9 +34,9 @@ __global__ __launch_bounds__(64 * WAVES) void int4_rows_kernel(const typename El
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int row = lane & 15, quarter = lane >> 4;
-    // blocks of rows that read the same weights follow each other on an XCD
-    const int turn = blockIdx.x >> 3, tile0 = (turn / row_blocks * 8 + (blockIdx.x & 7)) * NT, m0 = turn % row_blocks * ROWS;
-    if (tile0 >= w.output_tiles) return;
+    // an eighth of the work to each of the eight XCDs, blocks of rows that read the same weights one behind the other
+    const int each = gridDim.x >> 3, rest = gridDim.x & 7, xcd = blockIdx.x & 7, turn = xcd * each + min(xcd, rest) + (blockIdx.x >> 3);
+    const int tile0 = turn / row_blocks * NT, m0 = turn % row_blocks * ROWS;
     const bool fits = matches(w);
     const uint32_t one = in_lanes(P::kOne);
 
@@ -203,7 +203,7 @@ __global__ __launch_bounds__(64 * WAVES) void int4_rows_kernel(const typename El
 template <int XT, int GROUP, bool ZEROS, bool BF16, int ROWS, int NT, int WAVES>
 hipError_t launch(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
     const int row_blocks = ceil_div(o.M, ROWS);
-    const long long blocks = (long long)ceil_div(ceil_div(w.output_tiles, NT), 8) * 8 * row_blocks;
+    const long long blocks = (long long)ceil_div(w.output_tiles, NT) * row_blocks;
     int4_rows_kernel<XT, GROUP, ZEROS, BF16, ROWS, NT, WAVES><<<(unsigned)blocks, 64 * min(WAVES, w.input_tiles), 0, s>>>(
         static_cast<const typename Element<XT>::type*>(x), x_stride, w, o, row_blocks);
     return hipGetLastError();

@@ -196,7 +196,7 @@ __device__ inline void store_outputs(const Int4Output& o, int m, int n, v4f v, f
     const int count = min(4, o.N - n);
     if (o.type == WQ_F32) {
         float* y = static_cast<float*>(o.y) + at;
-        if ((o.N & 3) == 0) store_unaligned<4>(y, v4f{r[0], r[1], r[2], r[3]});
+        if (count == 4) store_unaligned<4>(y, v4f{r[0], r[1], r[2], r[3]});
         else
             for (int i = 0; i < count; ++i) y[i] = r[i];
         return;
@@ -206,7 +206,7 @@ __device__ inline void store_outputs(const Int4Output& o, int m, int n, v4f v, f
     for (int i = 0; i < 4; ++i)
         h[i] = o.type == WQ_F16 ? __builtin_bit_cast(uint16_t, (_Float16)r[i]) : __builtin_bit_cast(uint16_t, (__bf16)r[i]);
     uint16_t* y = static_cast<uint16_t*>(o.y) + at;
-    if ((o.N & 3) == 0) store_unaligned<2>(y, v2u{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16});
+    if (count == 4) store_unaligned<2>(y, v2u{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16});
     else
         for (int i = 0; i < count; ++i) y[i] = h[i];
 }

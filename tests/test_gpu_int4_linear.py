@@ -55,7 +55,7 @@ def check(got, want, size, dtype, K, group):
 @pytest.mark.parametrize("dtype", [F16, BF16, I8])
 @pytest.mark.parametrize("group,zeros", [(32, True), (64, False), (128, True), (128, False)])
 @pytest.mark.parametrize("M,N,K", [(1, 16, 128), (1, 1, 1), (2, 17, 33), (16, 64, 256), (17, 40, 1000), (5, 129, 2049), (64, 48, 384),
-                                   (70, 33, 136), (131, 257, 640)])
+                                   (70, 33, 136), (131, 257, 640), (1000, 17, 96)])
 def test_every_size_against_64_bits(M, N, K, group, zeros, dtype):
     x, codes, scales, zero = make(M, N, K, group, dtype, zeros)
     packed = wg.pack_int4_weights(codes, scales, zero, group)

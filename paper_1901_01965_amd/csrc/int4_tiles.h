@@ -194,6 +194,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void int4_tiles_kernel(const typena
     }
     if (!fits) return;
     if (parts > 1) o.y = static_cast<float*>(o.y) + (size_t)blockIdx.y * o.M * o.N;
+    if constexpr (NT == 2) {
+        // (225 rows, 32 outputs of 128 inputs with bias and scales 12 us without, 8 with; for more outputs, and so more inputs as well, there are
+        // no registers)
+        float scale[kRowTiles];
+        v4f bias[NT];
+#pragma unroll
+        for (int mt = 0; mt < kRowTiles; ++mt) scale[mt] = row_scale(o, m0 + 16 * mt + row, P::kUnit);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) bias[nt] = bias_of(o, (n_tile0 + nt) * kTileOutputs + 4 * quarter);
+#pragma unroll
+        for (int mt = 0; mt < kRowTiles; ++mt)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+                store_outputs(o, m0 + 16 * mt + row, (n_tile0 + nt) * kTileOutputs + 4 * quarter, acc[nt][mt], scale[mt], bias[nt]);
+        return;
+    }
 #pragma unroll
     for (int mt = 0; mt < kRowTiles; ++mt)
 #pragma unroll

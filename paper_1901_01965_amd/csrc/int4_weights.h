@@ -180,19 +180,8 @@ struct Int4Output {
     int type, M, N, relu;
 };
 
-// unit: the operands'.
-__device__ inline void store_outputs(const Int4Output& o, int m, int n, v4f v, float unit) {
-    if (m >= o.M || n >= o.N) return;
-    v *= unit;
-    if (o.x_scale) v *= o.x_scale[m];
+__device__ inline void store_rounded(const Int4Output& o, int m, int n, const float (&r)[4]) {
     const long long at = (long long)m * o.N + n;
-    float r[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        r[i] = v[i];
-        if (o.bias && n + i < o.N) r[i] += o.bias[n + i];
-        if (o.relu) r[i] = r[i] < 0.0f ? 0.0f : r[i];   // keeps NaN
-    }
     const int count = min(4, o.N - n);
     if (o.type == WQ_F32) {
         float* y = static_cast<float*>(o.y) + at;
@@ -209,6 +198,42 @@ __device__ inline void store_outputs(const Int4Output& o, int m, int n, v4f v, f
     if (count == 4) store_unaligned<2>(y, v2u{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16});
     else
         for (int i = 0; i < count; ++i) y[i] = h[i];
+}
+
+// unit: the operands'.
+__device__ inline void store_outputs(const Int4Output& o, int m, int n, v4f v, float unit) {
+    if (m >= o.M || n >= o.N) return;
+    v *= unit;
+    if (o.x_scale) v *= o.x_scale[m];
+    float r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r[i] = v[i];
+        if (o.bias && n + i < o.N) r[i] += o.bias[n + i];
+        if (o.relu) r[i] = r[i] < 0.0f ? 0.0f : r[i];   // keeps NaN
+    }
+    store_rounded(o, m, n, r);
+}
+
+// The same where many are stored: behind a store, every load of a scale or a bias would be waited for by itself, so they come first.
+__device__ inline float row_scale(const Int4Output& o, int m, float unit) { return o.x_scale ? unit * o.x_scale[min(m, o.M - 1)] : unit; }
+__device__ inline v4f bias_of(const Int4Output& o, int n) {
+    v4f b = {};
+    if (o.bias)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b[i] = o.bias[min(n + i, o.N - 1)];
+    return b;
+}
+__device__ inline void store_outputs(const Int4Output& o, int m, int n, v4f v, float scale, v4f bias) {
+    if (m >= o.M || n >= o.N) return;
+    float r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r[i] = v[i] * scale;
+        if (o.bias) r[i] += bias[i];
+        if (o.relu) r[i] = r[i] < 0.0f ? 0.0f : r[i];
+    }
+    store_rounded(o, m, n, r);
 }
 
 hipError_t launch_int4_pack(const uint8_t* codes, const void* scales, const uint8_t* zeros, const Int4Weights& w, uint8_t* blob, hipStream_t s);

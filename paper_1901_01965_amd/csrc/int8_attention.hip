@@ -64,7 +64,7 @@ hipError_t launch_join(const AttentionArgs& a, const AttentionPlan& p, int type,
     return head_dim == 64 ? join<WQ_BF16, 64>(a, p, s) : head_dim == 128 ? join<WQ_BF16, 128>(a, p, s) : join<WQ_BF16, 256>(a, p, s);
 }
 
-AttentionPlan plan_attention(int rows, int heads, int kv_heads, int head_dim, int block, int width, int sequences, bool has_starts) {
+AttentionPlan plan_attention(int rows, int heads, int kv_heads, int head_dim, int block, int width, int sequences, bool has_starts, int window) {
     AttentionPlan p;
     const int group = heads / kv_heads;
     // few rows of a sequence for the kernel that reads the cache once for 16 rows; more for the one that shares it among many
@@ -82,13 +82,17 @@ AttentionPlan plan_attention(int rows, int heads, int kv_heads, int head_dim, in
     // what is left of the longest sequences at the end is small (64 sequences, 8 heads of keys, 500 to 8192 tokens: 140 us unsplit, 127
     // so; one of 30000 among 1500: 358 and 126; all of 4096: 102 and 113).
     // Many rows: as many as give every compute unit two workgroups, but none a third, of eight steps, since a part's sums go through
-    // memory; two parts, which gain least, of 32 (5 heads of keys, 4 of queries each, 353 rows at 4381 tokens: 147 us unsplit, 47 in 8
-    // parts, 57 in 9; 600 rows at 600 tokens: 29 unsplit, 36 in parts of four steps; 8 heads, 1024 at 1024: 43 and 58 in 2 of eight).
+    // memory; two parts, which gain least, of 32; of few tiles two steps (5 heads of keys, 4 of queries each, 353 rows at 4381 tokens: 147
+    // us unsplit, 47 in 8 parts, 57 in 9; 8 heads, 600 rows at 600 tokens: 29 unsplit, 36 in parts of four steps; 1024 at 1024: 43 and 58
+    // in 2 of eight; but 2 heads, 100 at 2000: 27 in parts of eight steps, 18 of two).
     const bool enough = !p.many && tiles >= kComputeUnits;
     const long long likely = max(((long long)ceil_div(rows, p.unit) + (sequences - 1) / 2) * kv_heads, 1ll);   // tiles that have rows
     const long long wanted = enough ? 4 : p.many ? max(2 * kComputeUnits / likely, 1ll) : max(kComputeUnits / tiles, 1ll);
-    p.least_steps = p.many ? (wanted > 2 ? 8 : 32) : enough ? 8 : 4;
-    const long long most = min(max(((long long)width * block / kStep + p.least_steps / 2) / p.least_steps, 1ll), (long long)kMostParts);
+    p.least_steps = p.many ? (likely <= kComputeUnits / 4 ? 2 : wanted > 2 ? 8 : 32) : enough ? 8 : 4;
+    // steps that a tile can have: its table's, or those of its rows' windows
+    long long steps = (long long)width * block / kStep;
+    if (window > 0) steps = min(steps, ((long long)window + p.unit) / kStep + 2);
+    const long long most = min(max((steps + p.least_steps / 2) / p.least_steps, 1ll), (long long)kMostParts);
     p.splits = (int)min(wanted, most);
     p.workspace = p.splits > 1 ? (size_t)tiles * p.splits * p.tile_rows * (head_dim + 2) * sizeof(float) : 0;
     return p;
@@ -106,7 +110,7 @@ size_t int8_cache_attention_workspace_bytes(int rows, int heads, int kv_heads, i
                                             int sequences, int has_starts) {
     if (rows <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || table_width <= 0 || sequences <= 0) return 0;
     if ((head_dim != 64 && head_dim != 128 && head_dim != 256) || (block != 16 && block != 32 && block != 64 && block != 128)) return 0;
-    return plan_attention(rows, heads, kv_heads, head_dim, block, table_width, sequences, has_starts != 0).workspace;
+    return plan_attention(rows, heads, kv_heads, head_dim, block, table_width, sequences, has_starts != 0, 0).workspace;   // a window only takes from it
 }
 
 int int8_cache_attention(const void* q_dev, long long q_stride, int type, int rows, int heads, const int8_t* cache_k_dev,
@@ -124,7 +128,7 @@ int int8_cache_attention(const void* q_dev, long long q_stride, int type, int ro
     if (q_stride < (long long)heads * head_dim || out_stride < (long long)heads * head_dim) return WG_EINVAL;
     if (empty) return WG_OK;
     if (!q_dev || !out_dev || !aligned(q_dev, 2) || !aligned(out_dev, 2)) return WG_EINVAL;
-    const AttentionPlan p = plan_attention(rows, heads, kv_heads, head_dim, block, table_width, sequences, starts_dev != nullptr);
+    const AttentionPlan p = plan_attention(rows, heads, kv_heads, head_dim, block, table_width, sequences, starts_dev != nullptr, window);
     // workgroups of either launch, which the kernel for many rows has along one dimension
     if (p.items * max(p.splits, p.splits > 1 ? p.tile_rows : 1) > kMostItems || (p.many && p.items * kv_heads * p.splits > kMostItems)) return WG_EUNSUPPORTED;
     if (p.workspace > 0) {

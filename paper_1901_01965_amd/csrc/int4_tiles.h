@@ -1,12 +1,13 @@
-// y = x W^T with 4-bit weights for many rows: the matrix cores' rate bounds it.
+// y = x W^T with 4-bit weights for many rows: the matrix cores' rate bounds it (4096 rows through 4096 x 8192, float16 in groups of 128: 232 us,
+// 1.18 PFLOP/s; int8 184).
 //
 // A workgroup computes 64 NT outputs by 128 rows, each of its four waves 16 NT of the outputs by all rows, over the inputs by tiles
 // of 128.  Codes go through the wave's own part of the LDS as they lie and become operands in registers, once per workgroup; activations
 // are shared by the waves through LDS, where the 16-byte piece c of a row r lies at c ^ (r & 15), which keeps the reads of 16 rows'
 // pieces free of bank conflicts.  Both travel there without registers, the next tile's while this one is multiplied.  A group's
 // products are summed apart and enter the result by one multiply-add with the scale; those of 16 rows are done between the products of
-// the next 16.  While a wave multiplies it goes ahead of the other one of its SIMD, which then unpacks codes meanwhile (270 -> 257 us
-// for 4096 rows through 4096 x 8192).
+// the next 16.  While a wave multiplies it goes ahead of the other one of its SIMD, which then unpacks codes meanwhile (5% of
+// that time).
 //
 // bfloat16 activations come here as float16 (int4_linear.hip): unpacked codes then take their zero point off by a packed addition, for
 // which bfloat16 has no instruction (the product with a constant that stands in for it elsewhere took a fifth of the matrix cores).
@@ -234,9 +235,10 @@ inline long long rounds(const Int4Weights& w, const Int4Output& o, int nt) {
 template <int XT>
 hipError_t launch_tiles_of(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, int parts, hipStream_t s) {
     return with_weights(w, [&](auto group, auto zeros, auto bf16) {
-        // More tiles of outputs a wave read LDS less often per product, in coarser rounds.  Measured against two, alike in rounds: three
-        // 0.82 (float16 in groups of 128, whose operands leave no room for four: 4096 rows through 4096 x 8192 260 against 280 us, 8192
-        // through 4096 x 28672 1660 and 1797; but 2048 through 4096 x 4096 80 and 70), four 0.92 (int8 183 and 197, groups of 64 264 and 295).
+        // More tiles of outputs a wave read LDS less often per product, in coarser rounds: three of float16 in groups of 128, whose operands leave no
+        // room for four, which cost 1.23 of two's time a round, four otherwise, 1.84.  (Three against two: 4096 rows through 4096 x 8192
+        // 237 and 250 us, 8192 through 4096 x 28672 1546 and 1735, but 2048 through 4096 x 4096 72 and 66; four against two: int8, 4096
+        // through 4096 x 8192, 184 and 217, 1200 float16 rows in groups of 32 through 448 x 20000 58 and 65.)
         constexpr int kMore = XT == WQ_F16 && group() == 128 ? 3 : 4;
         constexpr double kCost = kMore == 3 ? 0.82 * 1.5 : 0.92 * 2;
         if (parts == 1 && rounds(w, o, kMore) * kCost < rounds(w, o, 2)) return launch<XT, group(), zeros(), bf16(), kMore>(x, x_stride, w, o, 1, s);

@@ -2,7 +2,8 @@
 //
 // A workgroup takes 16 rows that read the same head of keys (the heads of a group, times a few tokens) and a part of the sequence's
 // tokens; its four waves take 64 tokens in turn and join at the end, parts of a sequence join in a second kernel.  One pass: running
-// largest score and sum per row.  The cache's bytes bound it, so a wave's loads are whole: 16 bytes a lane, of keys along head_dim, of
+// largest score and sum per row.  The cache's bytes bound it (64 rows at 500 to 8192 tokens, 8 heads of 128: 124 us, 4.6 TB/s; one at 131071
+// 58), so a wave's loads are whole: 16 bytes a lane, of keys along head_dim, of
 // values along the tokens, and the next 64 tokens are on their way while these are worked on.
 //
 // Both products run on the matrix cores with codes turned into float16, exactly.  Scores are formed as K Q^T: in the 16x16 result a

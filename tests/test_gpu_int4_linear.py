@@ -65,6 +65,17 @@ def test_every_size_against_64_bits(M, N, K, group, zeros, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16, I8])
+@pytest.mark.parametrize("group,zeros", [(32, True), (64, False), (128, True)])
+@pytest.mark.parametrize("N,K", [(4099, 2200), (9000, 1290), (16900, 650)])
+@pytest.mark.parametrize("M", [1, 4, 5, 16, 31, 70])
+def test_few_rows_of_many_outputs(M, N, K, group, zeros, dtype):
+    """More tiles of outputs than compute units: a workgroup takes several, of fewer waves; the last ones end inside both."""
+    x, codes, scales, zero = make(M, N, K, group, dtype, zeros, seed=14)
+    got = wg.int4_linear(x, wg.pack_int4_weights(codes, scales, zero, group))
+    check(got, *reference(x, codes, scales, zero, group), dtype, K, group)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, I8])
 @pytest.mark.parametrize("group,zeros", [(32, False), (64, True), (128, False), (128, True)])
 @pytest.mark.parametrize("M,N,K", [(1101, 8200, 384), (131, 11001, 1100), (100, 20001, 2000), (300, 5003, 1000)])
 def test_enough_rows_and_outputs_for_tiles(M, N, K, group, zeros, dtype):

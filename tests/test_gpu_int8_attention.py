@@ -125,6 +125,20 @@ def test_long_sequences(heads, kv_heads, rows):
     check(got, *reference(q, cache, table, lengths, begins, 1 / math.sqrt(dim)))
 
 
+@pytest.mark.parametrize("dim,block", [(64, 16), (128, 64), (256, 128)])
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (12, 2)])
+@pytest.mark.parametrize("lengths,news,causal,window", [
+    ([752], [127], True, 0), ([3589, 0, 2322], [105, 0, 90], True, 0), ([2000], [300], True, 53), ([2000, 700], [300, 70], True, 700),
+    ([1537, 90], [130, 90], False, 0), ([129], [129], True, 0)])
+def test_parts_of_sequences_that_many_rows_ask(lengths, news, causal, window, heads, kv_heads, dim, block):
+    blocks = sum(-(-n // block) + 1 for n in lengths)
+    cache = random_cache(blocks, kv_heads, dim, block, 21)
+    table, on_gpu, starts, begins = batch(lengths, news, block, blocks, extra=5)
+    q = queries(begins[-1], heads, dim, BF16, seed=5)
+    got = wg.int8_cache_attention(q, cache, table, on_gpu, starts, causal=causal, window=window)
+    check(got, *reference(q, cache, table, lengths, begins, dim ** -0.5, causal, window))
+
+
 @pytest.mark.parametrize("rows", [1, 2, 90])
 def test_scales_of_unlike_sizes_and_one_far_larger_score(rows):
     """Blocks whose scales differ by 2^20, rise and fall; rows whose weight lies on one token late in the sequence."""

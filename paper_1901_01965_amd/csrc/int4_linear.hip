@@ -121,11 +121,12 @@ struct Int4Plan {
     size_t factors, sums, total;     // offsets of the factors and of the parts' sums, and all in bytes
 };
 // How long either kernel takes, in us, to about a quarter (measured at 33 to 4000 rows, 16 to 30000 outputs of 32 to 28672 inputs).  For few rows:
-// a workgroup to a compute unit at a time, for 16 or 32 outputs of 32 rows, whose eight waves share the tiles of inputs.
+// a workgroup to a compute unit at a time, for 16, 32 or 64 outputs of 32 rows, whose eight waves share the tiles of inputs.
 double rows_time(int M, int N, int K) {
-    const int tiles = ceil_div(N, kTileOutputs);
-    const long long workgroups = (long long)ceil_div(M, 32) * (tiles < kComputeUnits ? tiles : ceil_div(tiles, 2));
-    return 2.0 + (workgroups + kComputeUnits - 1) / kComputeUnits * (2.2 + 1.05 * ceil_div(ceil_div(K, kTileInputs), 8));
+    const int tiles = ceil_div(N, kTileOutputs), blocks = ceil_div(M, 32);
+    const bool wide = tiles >= kComputeUnits && (long long)blocks * tiles >= 4 * kComputeUnits;
+    const long long workgroups = (long long)blocks * (wide ? ceil_div(tiles, 4) : tiles < kComputeUnits ? tiles : ceil_div(tiles, 2));
+    return 2.0 + (workgroups + kComputeUnits - 1) / kComputeUnits * (2.2 + (wide ? 1.85 : 1.05) * ceil_div(ceil_div(K, kTileInputs), 8));
 }
 // For many: 1.2 us a tile of inputs as long as no two workgroups share a compute unit, a little less each if they do; parts of the inputs
 // are written, read again and added up by a launch more, and a copy of the rows is another.  (Their best number, one, and the kernel for few

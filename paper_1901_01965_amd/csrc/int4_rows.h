@@ -31,7 +31,11 @@ __global__ __launch_bounds__(64 * WAVES) void int4_rows_kernel(const typename El
     // one, reads would wait for what is on its way into the other half
     typedef v4u Held[kHeld * kPieces];
     __shared__ Held even[WAVES], odd[WAVES];
-    __shared__ v4f sums[WAVES][NT * MT][64];
+    // the waves' sums take the place of what was held, where there is room for them
+    constexpr bool kInPlace = NT * MT * 64 <= kHeld * kPieces;
+    typedef v4u Sums[NT * MT][64];
+    __shared__ Sums apart[kInPlace ? 1 : WAVES];
+    Sums* const sums = kInPlace ? reinterpret_cast<Sums*>(even) : apart;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int row = lane & 15, quarter = lane >> 4;
@@ -186,17 +190,18 @@ __global__ __launch_bounds__(64 * WAVES) void int4_rows_kernel(const typename El
         load_codes(now, whole_tiles);
         multiply(now, mine);
     }
+    if (kInPlace) __syncthreads();
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) sums[wave][nt * MT + mt][lane] = acc[nt][mt];
+        for (int mt = 0; mt < MT; ++mt) sums[wave][nt * MT + mt][lane] = __builtin_bit_cast(v4u, acc[nt][mt]);
     __syncthreads();
     if (!fits) return;
     for (int e = threadIdx.x; e < NT * MT * 64; e += blockDim.x) {
         const int tile = e >> 6, l = e & 63, r = 16 * (tile % MT) + (l & 15);
         if (r >= ROWS) continue;
-        v4f total = sums[0][tile][l];
-        for (int v = 1; v < waves; ++v) total += sums[v][tile][l];
+        v4f total = __builtin_bit_cast(v4f, sums[0][tile][l]);
+        for (int v = 1; v < waves; ++v) total += __builtin_bit_cast(v4f, sums[v][tile][l]);
         store_outputs(o, m0 + r, (tile0 + tile / MT) * kTileOutputs + 4 * (l >> 4), total, P::kUnit);
     }
 }
@@ -213,7 +218,8 @@ hipError_t launch(const void* x, long long x_stride, const Int4Weights& w, const
 // How many tiles of outputs a workgroup takes and how many waves: what keeps about 16 waves on every compute unit, with the activations
 // read by as few workgroups as that allows.  (Cold weights; 16 rows: 4096 outputs of 25088 int8 inputs 16.6 us with one tile and 16 waves, 22.3
 // with eight; 8192 of 8192 13.3 with two tiles, 16.6 with one; 16384 of 4096 10.7 with four, 12.8 with two.  One row: 28672 of 4096 14.9
-// with four waves, 16.6 with eight.  32 rows: 8192 of 8192 15.7 with two tiles, 23.5 with one.)
+// with four waves, 16.6 with eight.  32 rows: 8192 of 8192 15.7 with two tiles, 23.5 with one; 64: 19.5 with four, 27.8 with two; 64 rows in
+// groups of 32, 16384 of 4096, 50 with four, 38 with two.)
 template <int XT>
 hipError_t launch_rows_of(const void* x, long long x_stride, const Int4Weights& w, const Int4Output& o, hipStream_t s) {
     return with_weights(w, [&](auto group, auto zeros, auto bf16) {
@@ -229,7 +235,10 @@ hipError_t launch_rows_of(const void* x, long long x_stride, const Int4Weights& 
                            : tiles <= 4 * kComputeUnits ? run(four, two, eight) : run(four, two, four);
         if (o.M <= 16) return tiles <= kComputeUnits ? run(sixteen, one, sixteen) : tiles < 2 * kComputeUnits ? run(sixteen, one, eight)
                             : tiles < 4 * kComputeUnits ? run(sixteen, two, eight) : run(sixteen, four, eight);
-        return tiles < kComputeUnits ? run(thirty_two, one, eight) : run(thirty_two, two, eight);
+        if (tiles < kComputeUnits) return run(thirty_two, one, eight);
+        if constexpr (group() >= 64)   // the factors of more groups would leave no registers
+            if ((long long)ceil_div(o.M, 32) * tiles >= 4 * kComputeUnits) return run(thirty_two, four, eight);
+        return run(thirty_two, two, eight);
     });
 }
 

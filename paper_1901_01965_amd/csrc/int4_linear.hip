@@ -128,13 +128,14 @@ double rows_time(int M, int N, int K) {
     const long long workgroups = (long long)blocks * (wide ? ceil_div(tiles, 4) : tiles < kComputeUnits ? tiles : ceil_div(tiles, 2));
     return 2.0 + (workgroups + kComputeUnits - 1) / kComputeUnits * (2.2 + (wide ? 1.85 : 1.05) * ceil_div(ceil_div(K, kTileInputs), 8));
 }
-// For many: 1.2 us a tile of inputs as long as no two workgroups share a compute unit, a little less each if they do; parts of the inputs
-// are written, read again and added up by a launch more, and a copy of the rows is another.  (Their best number, one, and the kernel for few
-// rows: 1661 rows, 1024 outputs of 28672 inputs 132, 318 and 821 us; 256, 4096 of 4096 24, 38 and 29; 128, 4096 of 14336 29, 120 and 39;
-// but 64, 4096 of 4096 20, 42 and 10.)
+// For many: 1.2 us a tile of inputs as long as no two workgroups share a compute unit, 1.4 times that for two, which is as many as run there at
+// a time; parts of the inputs are written, read again and added up by a launch more, and a copy of the rows is another.  (Their best
+// number, one, and the kernel for few rows: 1661 rows, 1024 outputs of 28672 inputs 136, 317 and 808 us; 400, 4096 of 4096 31, 40 and
+// 33; 256, 8192 of 8192 50, 72 and 65; but 256, 4096 of 4096 26, 40 and 20; 300, 14336 of 4096 is best in one, 55 and 76.)
 double tiles_time(int M, int N, int K, int parts, bool copy) {
     const long long workgroups = (long long)ceil_div(M, kTileRows) * ceil_div(N, 8 * kTileOutputs) * parts;
-    const double at_a_time = workgroups <= kComputeUnits ? 1.0 : 0.9 * ((workgroups + kComputeUnits - 1) / kComputeUnits);
+    const long long deep = (workgroups + kComputeUnits - 1) / kComputeUnits;
+    const double at_a_time = 1.4 * (deep / 2) + deep % 2;
     const double inputs = (double)ceil_div(ceil_div(K, kTileInputs), parts) * 1.2 * at_a_time;
     return 3.0 + inputs + (parts > 1 ? 6.0 + 1.3e-6 * parts * M * N : 0.0) + (copy ? 4.0 : 0.0);
 }

@@ -33,9 +33,11 @@ __global__ __launch_bounds__(64 * WAVES) void int4_rows_kernel(const typename El
     __shared__ Held even[WAVES], odd[WAVES];
     // the waves' sums take the place of what was held where there would be no room for both
     constexpr bool kInPlace = ROWS == 32 && NT * MT * 64 <= kHeld * kPieces;
-    typedef v4u Sums[NT * MT][64];
-    __shared__ Sums apart[kInPlace ? 1 : WAVES];
-    Sums* const sums = kInPlace ? reinterpret_cast<Sums*>(even) : apart;
+    __shared__ v4f apart[kInPlace ? 1 : WAVES][NT * MT][64];
+    auto sums = [&](int v, int tile, int l) -> v4f& {
+        if constexpr (kInPlace) return reinterpret_cast<v4f*>(even)[(v * NT * MT + tile) * 64 + l];
+        else return apart[v][tile][l];
+    };
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int row = lane & 15, quarter = lane >> 4;
@@ -192,18 +194,18 @@ __global__ __launch_bounds__(64 * WAVES) void int4_rows_kernel(const typename El
         load_codes(now, whole_tiles);
         multiply(now, mine);
     }
-    if (kInPlace) __syncthreads();
+    if constexpr (kInPlace) __syncthreads();
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) sums[wave][nt * MT + mt][lane] = __builtin_bit_cast(v4u, acc[nt][mt]);
+        for (int mt = 0; mt < MT; ++mt) sums(wave, nt * MT + mt, lane) = acc[nt][mt];
     __syncthreads();
     if (!fits) return;
     for (int e = threadIdx.x; e < NT * MT * 64; e += blockDim.x) {
         const int tile = e >> 6, l = e & 63, r = 16 * (tile % MT) + (l & 15);
         if (r >= ROWS) continue;
-        v4f total = __builtin_bit_cast(v4f, sums[0][tile][l]);
-        for (int v = 1; v < waves; ++v) total += __builtin_bit_cast(v4f, sums[v][tile][l]);
+        v4f total = sums(0, tile, l);
+        for (int v = 1; v < waves; ++v) total += sums(v, tile, l);
         store_outputs(o, m0 + r, (tile0 + tile / MT) * kTileOutputs + 4 * (l >> 4), total, P::kUnit);
     }
 }

@@ -1,5 +1,5 @@
-// y = x W^T with 4-bit weights for few rows: the weights' bytes are read once, everything else stays beside them (one row through 4096 x 16384 9.5
-// us, 3.7 TB/s; 16 rows through 8192 x 8192 10, int8 through 25088 x 4096 12, 4.4 TB/s).
+// y = x W^T with 4-bit weights for few rows: the weights' bytes are read once, everything else stays beside them (one row through 4096 x 16384 9.2
+// us, 3.8 TB/s; 16 rows through 8192 x 8192 10, int8 through 25088 x 4096 12, 4.4 TB/s).
 //
 // A workgroup takes 16 NT outputs and up to ROWS rows; its up to WAVES waves share the inputs out by tiles of 128 and add their sums up in LDS at the
 // end, in the order of the waves.  The matrix cores multiply (rows beyond the last are copies of others and are not stored): a word of
